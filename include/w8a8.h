@@ -498,6 +498,160 @@ w8a8_status w8a8_attn_decode_bf16(const void* qkv, int n_heads, int64_t pos, int
                                   void* k_rows, void* v_rows, int64_t t_max, void* out, void* ws,
                                   size_t ws_bytes, w8a8_stream_t stream);
 
+/* ---------------------------------------------------------------- rotary positions */
+
+/* Rotary positions: pair j of a head of the token at position p is turned by
+   the angle p * freq[j],
+     (a, b) -> scale * (a cos - b sin, b cos + a sin),
+   for the first rot_dim elements of the head; the others pass unchanged.
+   W8A8_ROPE_HALF pairs elements j and j + rot_dim / 2, W8A8_ROPE_INTERLEAVED
+   elements 2 j and 2 j + 1.  Angles are binary64, products binary32, results
+   rounded once. */
+enum { W8A8_ROPE_HALF = 0, W8A8_ROPE_INTERLEAVED = 1 };
+typedef struct {
+    int64_t head_dim;    /* a multiple of 16, at most 1024 */
+    int64_t rot_dim;     /* a multiple of 16, 16 .. head_dim */
+    int layout;          /* W8A8_ROPE_* */
+    const double* freq;  /* DEVICE double[rot_dim / 2], radians a position */
+    float scale;         /* factor on cosine and sine (1 without scaling) */
+} w8a8_rope_desc;
+
+/* Frequencies of the pairs, freq[j] = theta^(-2 j / rot_dim), and their usual
+   scalings for contexts longer than the trained one (factor >= 1):
+     W8A8_ROPE_PLAIN   none (factor is not read);
+     W8A8_ROPE_LINEAR  every frequency divided by factor;
+     W8A8_ROPE_NTK     theta * factor^(rot_dim / (rot_dim - 2)) as the base, so
+                       that the slowest pair is slowed by factor and the fastest
+                       is not (rot_dim >= 4);
+     W8A8_ROPE_YARN    by pair (arXiv 2309.00071): pairs that turn more than 32
+                       times over `original` positions keep their frequency,
+                       those that turn less than once are divided by factor, a
+                       linear ramp over j between them; scale = 1 + 0.1 ln(factor).
+   freq: HOST double[rot_dim / 2]; scale: HOST float[1], the descriptor's factor
+   (1 but for YARN).  Host-only: returns 0, or -1 for NULL arguments, an odd or
+   non-positive rot_dim, an unknown kind, theta <= 1, factor < 1 or (YARN)
+   original < 1. */
+enum { W8A8_ROPE_PLAIN = 0, W8A8_ROPE_LINEAR = 1, W8A8_ROPE_NTK = 2, W8A8_ROPE_YARN = 3 };
+int w8a8_rope_frequencies(int64_t rot_dim, double theta, int kind, double factor, double original,
+                          double* freq, float* scale);
+
+/* Rotates n_heads heads of each row: head h of row r starts at x + r * ldx +
+   h * head_dim elements and goes to y + r * ldy + h * head_dim.  dtype: bf16 or
+   f32, of x and y.  pos: DEVICE int32[rows], the rows' positions.  y may be x
+   with ldy == ldx (in place); elements of a row past its heads are not
+   written.  E.g. the n_heads + 1 query and key heads of the fused QKV row that
+   w8a8_attn_decode takes (n_heads = its heads + 1).  ldx, ldy >= n_heads *
+   head_dim and multiples of 8 (EINVAL otherwise); EUNSUPPORTED for other head
+   or rotated widths, layouts and dtypes. */
+w8a8_status w8a8_rope(const w8a8_rope_desc* rope, const void* x, w8a8_dtype dtype, int64_t rows,
+                      int64_t n_heads, int64_t ldx, const int32_t* pos, void* y, int64_t ldy,
+                      w8a8_stream_t stream);
+
+/* ---------------------------------------------------------------- paged key/value cache */
+
+/* A key/value cache of n_pages pages that many sequences share: page i holds
+   `page` positions (a power of two, 16 .. 65536) of every key/value head,
+   row-major [n_pages][n_kv][page][head_dim] (head_dim 128 or 256), as INT8 codes
+   with one binary32 scale a row ([n_pages][n_kv][page], the rule of
+   w8a8_kv_quantize) or, with sk and sv NULL, as bf16 rows. */
+typedef struct {
+    int64_t n_pages, page, n_kv, head_dim;
+    void* k;
+    void* v;
+    float* sk;
+    float* sv;
+} w8a8_paged_kv;
+
+/* The sequences of one call, all arrays in DEVICE memory (a captured graph can
+   be replayed with new contents).  Sequence s has the new tokens q_start[s] ..
+   q_start[s + 1] - 1 of the call's rows (none if the two are equal; q_start
+   ascends); they are the last positions of its context of ctx_len[s]
+   positions: row r stands at position ctx_len[s] - (q_start[s + 1] - r).
+   Position p lies in page table[s * max_pages + p / page], slot p % page.  An
+   entry outside [0, n_pages) is a page that the sequence does not hold (given
+   back behind a window, or evicted): nothing is stored there, and its
+   positions are not attended.  Rows behind the last sequence (padding) are left
+   as they were.  max_q: no sequence has more new tokens (of one that has more,
+   w8a8_attn_paged may leave rows as they were).  A page may be in several
+   sequences' tables as long as no call stores to it. */
+typedef struct {
+    int64_t n_seqs, max_pages;
+    const int32_t* table;    /* [n_seqs][max_pages] */
+    const int32_t* q_start;  /* [n_seqs + 1] */
+    const int32_t* ctx_len;  /* [n_seqs] */
+    int64_t max_q;
+} w8a8_paged_batch;
+
+/* Stores the batch's new tokens in the cache.  qkv: bf16 rows (stride ld) of a
+   fused QKV projection, [n_heads | n_kv | n_kv] heads of head_dim: queries, keys,
+   values.  Queries and keys are rotated by rope (NULL: not rotated) at the
+   row's position in its sequence; the keys and values are stored at that
+   position, quantised from the binary32 rotated values (INT8 cache) or rounded
+   to bf16; the queries go to q (bf16, stride ldq), which may be qkv itself with
+   ldq == ld.  ld >= (n_heads + 2 n_kv) * head_dim, ldq >= n_heads * head_dim,
+   both multiples of 8.  rope->head_dim must be the cache's. */
+w8a8_status w8a8_kv_append(const void* qkv, int64_t rows, int64_t ld, int64_t n_heads,
+                           const w8a8_rope_desc* rope, const w8a8_paged_kv* kv,
+                           const w8a8_paged_batch* batch, void* q, int64_t ldq,
+                           w8a8_stream_t stream);
+
+/* The cached rows of the batch's new tokens, as bf16 (code * scale rounded
+   once): k, v are bf16 [rows][n_kv][head_dim]; zeros where the page is not held
+   (checks, and moving a sequence to another cache). */
+w8a8_status w8a8_kv_read(const w8a8_paged_kv* kv, const w8a8_paged_batch* batch, int64_t rows,
+                         void* k, void* v, w8a8_stream_t stream);
+
+/* Attention of the batch's new tokens over the cache, which holds their rows
+   already (w8a8_kv_append): head h of the token at position p of sequence s
+   reads key/value head h / (n_heads / n_kv) and attends the held positions j
+   with p - window < j <= p,
+     out = sum_j softmax_j(scale * q . k_j) v_j,
+   zeros where there is none.  q, out: bf16 rows x n_heads x head_dim, strides
+   ldq and ldo (multiples of 8).  n_heads: a multiple of n_kv.  window >= 1
+   (e.g. INT32_MAX for none), scale finite (1 / sqrt(head_dim) as a rule).  Sums
+   and softmax statistics are binary32.  Cached rows past ctx_len, before every
+   new token's window and in pages that are not held are never used.
+   ws: w8a8_attn_paged_workspace_bytes(...) bytes (may be NULL when that is 0);
+   ctx_max: the longest context that ctx_len may hold (max_pages * page at most
+   is used). */
+size_t w8a8_attn_paged_workspace_bytes(int64_t rows, int64_t n_heads, int64_t n_kv,
+                                       int64_t head_dim, int64_t n_seqs, int64_t max_q,
+                                       int64_t ctx_max);
+w8a8_status w8a8_attn_paged(const void* q, int64_t rows, int64_t ldq, int64_t n_heads,
+                            const w8a8_paged_kv* kv, const w8a8_paged_batch* batch,
+                            int64_t window, float scale, void* out, int64_t ldo, void* ws,
+                            size_t ws_bytes, w8a8_stream_t stream);
+
+/* ---------------------------------------------------------------- sampling */
+
+/* How each row's token is drawn.  An array (DEVICE, one entry a row) stands for
+   the value beside it where it is not NULL (its NaN entries: not above 0, or off). */
+typedef struct {
+    const float* temperature;  float temperature_all;  /* not above 0: the largest logit */
+    const int32_t* top_k;      int32_t top_k_all;      /* below 1 (or at least n): off */
+    const float* top_p;        float top_p_all;        /* 1 and more: off */
+    const float* min_p;        float min_p_all;        /* 0 and less: off */
+} w8a8_sample_desc;
+
+/* Draws one token for each row of logits (bf16 or f32, rows x n, stride ld >= n
+   elements, any alignment of a row) from the uniform number u[row] in [0, 1).
+   With w_i = exp((l_i - max_j l_j) / temperature), tokens in the order of
+   descending logits, the lower index first among equal ones, of which a prefix
+   is kept: top_k tokens; of these the shortest prefix whose weights add up to
+   top_p of theirs; of these the tokens with w_i >= min_p.  One token always
+   stays.  The token drawn is the first index i (in index order) with
+   sum_{kept j <= i} w_j > u sum_{kept} w_j; u below 0 or NaN draws the first
+   kept token, 1 and more the last.  Weights and sums are binary64.  Logits of -inf and NaN
+   are never drawn; of +inf ones each has weight 1 and all others 0.  A row with
+   nothing to draw gives token -1 (and prob 0).
+   u: DEVICE float[rows]; token: DEVICE int64[rows]; prob: DEVICE float[rows] or
+   NULL, w_token / sum_{kept} w.  n <= 2^24 (EUNSUPPORTED otherwise).
+   ws: w8a8_sample_workspace_bytes(rows, n, dtype) bytes (may be NULL when 0). */
+size_t w8a8_sample_workspace_bytes(int64_t rows, int64_t n, w8a8_dtype dtype);
+w8a8_status w8a8_sample(const w8a8_sample_desc* desc, const void* logits, w8a8_dtype dtype,
+                        int64_t rows, int64_t n, int64_t ld, const float* u, int64_t* token,
+                        float* prob, void* ws, size_t ws_bytes, w8a8_stream_t stream);
+
 /* ---------------------------------------------------------------- planner overrides */
 
 /* The GEMM planner picks tile shapes, K splits, streaming plans and the decode

@@ -2078,6 +2078,249 @@ w8a8_status w8a8_attn_decode_bf16(const void* qkv, int n_heads, int64_t pos, int
                    "attn_decode_bf16");
 }
 
+// ---------------------------------------------------------------- rotary positions, paged cache, sampling
+
+int w8a8_rope_frequencies(int64_t rot_dim, double theta, int kind, double factor, double original,
+                          double* freq, float* scale) {
+  if (!freq || !scale || rot_dim < 2 || rot_dim % 2 || rot_dim > (1 << 20)) return -1;
+  if (kind < W8A8_ROPE_PLAIN || kind > W8A8_ROPE_YARN || !(theta > 1.0) || !std::isfinite(theta)) return -1;
+  if (kind != W8A8_ROPE_PLAIN && !(factor >= 1.0 && std::isfinite(factor))) return -1;
+  if (kind == W8A8_ROPE_NTK && rot_dim < 4) return -1;
+  if (kind == W8A8_ROPE_YARN && !(original >= 1.0 && std::isfinite(original))) return -1;
+  const double r = (double)rot_dim, pi = 3.14159265358979323846;
+  if (kind == W8A8_ROPE_NTK) theta *= std::pow(factor, r / (r - 2.0));
+  // pair j turns original * theta^(-2 j / r) / (2 pi) times over the original context
+  auto pair_of = [&](double turns) { return r * std::log(original / (turns * 2.0 * pi)) / (2.0 * std::log(theta)); };
+  double lo = 0.0, hi = 1.0;
+  if (kind == W8A8_ROPE_YARN) {
+    lo = std::max(std::floor(pair_of(32.0)), 0.0);
+    hi = std::min(std::ceil(pair_of(1.0)), r - 1.0);
+  }
+  *scale = kind == W8A8_ROPE_YARN ? (float)(0.1 * std::log(factor) + 1.0) : 1.0f;
+  for (int64_t j = 0; j < rot_dim / 2; ++j) {
+    double f = std::pow(theta, -2.0 * (double)j / r);
+    if (kind == W8A8_ROPE_LINEAR) f /= factor;
+    if (kind == W8A8_ROPE_YARN) {
+      const double slow = std::min(std::max(((double)j - lo) / std::max(hi - lo, 1e-3), 0.0), 1.0);
+      f = f * (1.0 - slow) + f / factor * slow;
+    }
+    freq[j] = f;
+  }
+  return 0;
+}
+
+namespace {
+
+w8a8_status check_rope(const w8a8_rope_desc* r) {
+  REQUIRE(r, W8A8_EINVAL, "rope is NULL");
+  REQUIRE(r->freq && ((uintptr_t)r->freq & 7) == 0, W8A8_EINVAL, "rope->freq is NULL or not 8-byte aligned");
+  REQUIRE(r->head_dim >= 16 && r->head_dim <= 1024 && r->head_dim % 16 == 0, W8A8_EUNSUPPORTED,
+          "rope->head_dim must be a multiple of 16, 16 .. 1024");
+  REQUIRE(r->rot_dim >= 16 && r->rot_dim <= r->head_dim && r->rot_dim % 16 == 0, W8A8_EUNSUPPORTED,
+          "rope->rot_dim must be a multiple of 16, 16 .. head_dim");
+  REQUIRE(r->layout == W8A8_ROPE_HALF || r->layout == W8A8_ROPE_INTERLEAVED, W8A8_EUNSUPPORTED,
+          "rope->layout is neither half nor interleaved");
+  REQUIRE(std::isfinite(r->scale), W8A8_EINVAL, "rope->scale is not finite");
+  return W8A8_OK;
+}
+
+// rows and heads of a call: every grid made of them stays below 2^32 threads
+w8a8_status check_rows(int64_t rows, int64_t heads) {
+  REQUIRE(rows >= 1, W8A8_EINVAL, "rows < 1");
+  REQUIRE(heads >= 1, W8A8_EINVAL, "n_heads < 1");
+  REQUIRE(heads <= 4096 && rows <= (1 << 25) && rows * heads <= (1 << 27), W8A8_EUNSUPPORTED,
+          "more than 2^25 rows, 4096 heads or 2^27 heads of rows");
+  return W8A8_OK;
+}
+
+w8a8_status check_ld(int64_t ld, int64_t least, const char* name) {
+  REQUIRE(ld >= least && ld % 8 == 0 && ld <= ((int64_t)1 << 32), W8A8_EINVAL,
+          std::string(name) + " is below the row's width, above 2^32 or no multiple of 8");
+  return W8A8_OK;
+}
+
+w8a8_status check_paged(const w8a8_paged_kv* kv, const w8a8_paged_batch* b, PagedKv* k, PagedBatch* o) {
+  REQUIRE(kv, W8A8_EINVAL, "kv is NULL");
+  REQUIRE(b, W8A8_EINVAL, "batch is NULL");
+  REQUIRE(kv->head_dim == 128 || kv->head_dim == 256, W8A8_EUNSUPPORTED, "kv->head_dim must be 128 or 256");
+  REQUIRE(kv->page >= 16 && kv->page <= 65536 && (kv->page & (kv->page - 1)) == 0, W8A8_EUNSUPPORTED,
+          "kv->page must be a power of two, 16 .. 65536");
+  REQUIRE(kv->n_kv >= 1 && kv->n_pages >= 1, W8A8_EINVAL, "kv->n_kv or kv->n_pages < 1");
+  REQUIRE(kv->n_kv <= 4096 && kv->n_pages <= INT32_MAX, W8A8_EUNSUPPORTED, "kv->n_kv > 4096 or kv->n_pages > 2^31 - 1");
+  CHECK_PTR(kv->k);
+  CHECK_PTR(kv->v);
+  REQUIRE((kv->sk == nullptr) == (kv->sv == nullptr), W8A8_EINVAL, "kv->sk and kv->sv: both or neither");
+  if (kv->sk) {
+    CHECK_PTR(kv->sk);
+    CHECK_PTR(kv->sv);
+  }
+  REQUIRE(b->n_seqs >= 1 && b->max_pages >= 1 && b->max_q >= 1, W8A8_EINVAL,
+          "batch->n_seqs, batch->max_pages or batch->max_q < 1");
+  REQUIRE(b->n_seqs <= (1 << 20) && b->max_pages <= (1 << 30) / kv->page, W8A8_EUNSUPPORTED,
+          "more than 2^20 sequences or 2^30 positions");
+  for (const void* p : {(const void*)b->table, (const void*)b->q_start, (const void*)b->ctx_len})
+    REQUIRE(p && ((uintptr_t)p & 3) == 0, W8A8_EINVAL, "a batch array is NULL or not 4-byte aligned");
+  k->k = kv->k;
+  k->v = kv->v;
+  k->sk = kv->sk;
+  k->sv = kv->sv;
+  k->n_pages = (int)kv->n_pages;
+  k->n_kv = (int)kv->n_kv;
+  k->page_log2 = __builtin_ctzll((unsigned long long)kv->page);
+  o->table = b->table;
+  o->q_start = b->q_start;
+  o->ctx_len = b->ctx_len;
+  o->n_seqs = (int)b->n_seqs;
+  o->max_pages = (int)b->max_pages;
+  return W8A8_OK;
+}
+
+}  // namespace
+
+w8a8_status w8a8_rope(const w8a8_rope_desc* rope, const void* x, w8a8_dtype dtype, int64_t rows,
+                      int64_t n_heads, int64_t ldx, const int32_t* pos, void* y, int64_t ldy,
+                      w8a8_stream_t stream) {
+  g_last_error.clear();
+  CHECK(check_rope(rope));
+  CHECK_PTR(x);
+  CHECK_PTR(y);
+  REQUIRE(pos && ((uintptr_t)pos & 3) == 0, W8A8_EINVAL, "pos is NULL or not 4-byte aligned");
+  REQUIRE(dtype == W8A8_F32 || dtype == W8A8_BF16, W8A8_EUNSUPPORTED, "dtype must be f32 or bf16");
+  CHECK(check_rows(rows, n_heads));
+  CHECK(check_ld(ldx, n_heads * rope->head_dim, "ldx"));
+  CHECK(check_ld(ldy, n_heads * rope->head_dim, "ldy"));
+  REQUIRE(x != y || ldx == ldy, W8A8_EINVAL, "in place with two strides");
+  RopeParams p;
+  p.x = x;
+  p.y = y;
+  p.pos = pos;
+  p.freq = rope->freq;
+  p.rows = rows;
+  p.ldx = ldx;
+  p.ldy = ldy;
+  p.heads = (int)n_heads;
+  p.d = (int)rope->head_dim;
+  p.rot = (int)rope->rot_dim;
+  p.scale = rope->scale;
+  return hip_check(launch_rope(p, dtype == W8A8_BF16, rope->layout == W8A8_ROPE_INTERLEAVED, S(stream)), "rope");
+}
+
+w8a8_status w8a8_kv_append(const void* qkv, int64_t rows, int64_t ld, int64_t n_heads,
+                           const w8a8_rope_desc* rope, const w8a8_paged_kv* kv,
+                           const w8a8_paged_batch* batch, void* q, int64_t ldq,
+                           w8a8_stream_t stream) {
+  g_last_error.clear();
+  CHECK_PTR(qkv);
+  CHECK_PTR(q);
+  CHECK(check_rows(rows, n_heads));
+  AppendParams p;
+  CHECK(check_paged(kv, batch, &p.kv, &p.batch));
+  CHECK(check_ld(ld, (n_heads + 2 * kv->n_kv) * kv->head_dim, "ld"));
+  CHECK(check_ld(ldq, n_heads * kv->head_dim, "ldq"));
+  REQUIRE(qkv != q || ld == ldq, W8A8_EINVAL, "in place with two strides");
+  if (rope) {
+    CHECK(check_rope(rope));
+    REQUIRE(rope->head_dim == kv->head_dim, W8A8_EINVAL, "rope->head_dim is not the cache's");
+    p.freq = rope->freq;
+    p.rot = (int)rope->rot_dim;
+    p.scale = rope->scale;
+  }
+  p.qkv = (const uint16_t*)qkv;
+  p.q = (uint16_t*)q;
+  p.rows = rows;
+  p.ld = ld;
+  p.ldq = ldq;
+  p.n_heads = (int)n_heads;
+  return hip_check(launch_kv_append(p, (int)kv->head_dim, rope && rope->layout == W8A8_ROPE_INTERLEAVED, S(stream)),
+                   "kv_append");
+}
+
+w8a8_status w8a8_kv_read(const w8a8_paged_kv* kv, const w8a8_paged_batch* batch, int64_t rows,
+                         void* k, void* v, w8a8_stream_t stream) {
+  g_last_error.clear();
+  CHECK_PTR(k);
+  CHECK_PTR(v);
+  KvReadParams p;
+  CHECK(check_paged(kv, batch, &p.kv, &p.batch));
+  CHECK(check_rows(rows, kv->n_kv));
+  p.k_out = (uint16_t*)k;
+  p.v_out = (uint16_t*)v;
+  p.rows = rows;
+  return hip_check(launch_kv_read(p, (int)kv->head_dim, S(stream)), "kv_read");
+}
+
+size_t w8a8_attn_paged_workspace_bytes(int64_t rows, int64_t n_heads, int64_t n_kv,
+                                       int64_t head_dim, int64_t n_seqs, int64_t max_q,
+                                       int64_t ctx_max) {
+  return 0;
+}
+
+w8a8_status w8a8_attn_paged(const void* q, int64_t rows, int64_t ldq, int64_t n_heads,
+                            const w8a8_paged_kv* kv, const w8a8_paged_batch* batch,
+                            int64_t window, float scale, void* out, int64_t ldo, void* ws,
+                            size_t ws_bytes, w8a8_stream_t stream) {
+  g_last_error.clear();
+  CHECK_PTR(q);
+  CHECK_PTR(out);
+  CHECK(check_rows(rows, n_heads));
+  PagedAttnParams p;
+  CHECK(check_paged(kv, batch, &p.kv, &p.batch));
+  REQUIRE(n_heads % kv->n_kv == 0, W8A8_EINVAL, "n_heads is no multiple of kv->n_kv");
+  CHECK(check_ld(ldq, n_heads * kv->head_dim, "ldq"));
+  CHECK(check_ld(ldo, n_heads * kv->head_dim, "ldo"));
+  REQUIRE(window >= 1, W8A8_EINVAL, "window < 1");
+  REQUIRE(std::isfinite(scale), W8A8_EINVAL, "scale is not finite");
+  p.q = (const uint16_t*)q;
+  p.out = (uint16_t*)out;
+  p.rows = rows;
+  p.ldq = ldq;
+  p.ldo = ldo;
+  p.n_heads = (int)n_heads;
+  p.group = (int)(n_heads / kv->n_kv);
+  p.window = (int)std::min<int64_t>(window, 1 << 30);  // no position reaches it
+  p.scale_log2 = scale * 1.44269504088896341f;
+  return hip_check(launch_attn_paged(p, (int)kv->head_dim, S(stream)), "attn_paged");
+}
+
+size_t w8a8_sample_workspace_bytes(int64_t rows, int64_t n, w8a8_dtype dtype) { return 0; }
+
+w8a8_status w8a8_sample(const w8a8_sample_desc* desc, const void* logits, w8a8_dtype dtype,
+                        int64_t rows, int64_t n, int64_t ld, const float* u, int64_t* token,
+                        float* prob, void* ws, size_t ws_bytes, w8a8_stream_t stream) {
+  g_last_error.clear();
+  REQUIRE(desc, W8A8_EINVAL, "desc is NULL");
+  REQUIRE(dtype == W8A8_F32 || dtype == W8A8_BF16, W8A8_EUNSUPPORTED, "dtype must be f32 or bf16");
+  const uintptr_t elem = dtype == W8A8_BF16 ? 1 : 3;
+  REQUIRE(logits && ((uintptr_t)logits & elem) == 0, W8A8_EINVAL, "logits is NULL or not aligned to its type");
+  for (const void* p : {(const void*)desc->temperature, (const void*)desc->top_k, (const void*)desc->top_p,
+                        (const void*)desc->min_p, (const void*)prob})
+    REQUIRE(((uintptr_t)p & 3) == 0, W8A8_EINVAL, "an array is not 4-byte aligned");
+  REQUIRE(u && ((uintptr_t)u & 3) == 0, W8A8_EINVAL, "u is NULL or not 4-byte aligned");
+  REQUIRE(token && ((uintptr_t)token & 7) == 0, W8A8_EINVAL, "token is NULL or not 8-byte aligned");
+  REQUIRE(rows >= 1 && n >= 1, W8A8_EINVAL, "rows or n < 1");
+  REQUIRE(rows <= (1 << 20) && n <= kSampleMaxVocab, W8A8_EUNSUPPORTED, "more than 2^20 rows or 2^24 logits a row");
+  REQUIRE(ld >= n && ld <= ((int64_t)1 << 32), W8A8_EINVAL, "ld is below n or above 2^32");
+  REQUIRE(!std::isnan(desc->temperature_all) && !std::isnan(desc->top_p_all) && !std::isnan(desc->min_p_all),
+          W8A8_EINVAL, "temperature_all, top_p_all or min_p_all is NaN");
+  SampleParams p;
+  p.logits = logits;
+  p.u = u;
+  p.temperature = desc->temperature;
+  p.top_k = desc->top_k;
+  p.top_p = desc->top_p;
+  p.min_p = desc->min_p;
+  p.temperature_all = desc->temperature_all;
+  p.top_k_all = desc->top_k_all;
+  p.top_p_all = desc->top_p_all;
+  p.min_p_all = desc->min_p_all;
+  p.rows = rows;
+  p.n = n;
+  p.ld = ld;
+  p.token = token;
+  p.prob = prob;
+  return hip_check(launch_sample(p, dtype == W8A8_BF16, S(stream)), "sample");
+}
+
 }  // extern "C"
 
 // rows per workgroup of the many-row bf16 quantiser (declared in kernels.h)

@@ -301,4 +301,85 @@ hipError_t launch_attn_decode(AttnParams p, int nh, bool i8, int target, hipStre
 size_t attn_ws_bytes(int64_t rows, int target);  // workspace of one launch over `rows` rows
 size_t attn_ws_bytes_max(int64_t t_max);  // ... of any launch over at most t_max rows
 
+// ------------------------------------------------------------------ rotary positions, paged cache (rope.hip)
+
+struct RopeParams {
+  const void* x = nullptr;      // rows x heads x d (row stride ldx), bf16 or f32
+  void* y = nullptr;            // may alias x when ldy == ldx
+  const int32_t* pos = nullptr; // [rows]
+  const double* freq = nullptr; // [rot / 2] radians a position
+  int64_t rows = 0, ldx = 0, ldy = 0;
+  int heads = 0, d = 0, rot = 0;
+  float scale = 1.0f;
+};
+hipError_t launch_rope(const RopeParams& p, bool bf16, bool inter, hipStream_t st);
+
+// A cache of n_pages pages, [n_pages][n_kv][page][head_dim], page a power of two.
+struct PagedKv {
+  void* k = nullptr;            // INT8 codes, or bf16 where sk is null
+  void* v = nullptr;
+  float* sk = nullptr;          // [n_pages][n_kv][page]
+  float* sv = nullptr;
+  int n_pages = 0, n_kv = 0, page_log2 = 0;
+};
+// The sequences of a call: new tokens q_start[s] .. q_start[s + 1] - 1 of the
+// rows, the last ctx_len[s] positions ending with them.
+struct PagedBatch {
+  const int32_t* table = nullptr;    // [n_seqs][max_pages]
+  const int32_t* q_start = nullptr;  // [n_seqs + 1]
+  const int32_t* ctx_len = nullptr;  // [n_seqs]
+  int n_seqs = 0, max_pages = 0;
+};
+struct AppendParams {
+  const uint16_t* qkv = nullptr;  // rows x [n_heads | n_kv | n_kv] heads, stride ld
+  uint16_t* q = nullptr;          // rows x n_heads heads, stride ldq
+  const double* freq = nullptr;
+  int64_t rows = 0, ld = 0, ldq = 0;
+  int n_heads = 0, rot = 0;       // rot 0: no rotation
+  float scale = 1.0f;
+  PagedKv kv;
+  PagedBatch batch;
+};
+hipError_t launch_kv_append(const AppendParams& p, int head_dim, bool inter, hipStream_t st);
+struct KvReadParams {
+  uint16_t* k_out = nullptr;      // rows x n_kv x head_dim
+  uint16_t* v_out = nullptr;
+  int64_t rows = 0;
+  PagedKv kv;
+  PagedBatch batch;
+};
+hipError_t launch_kv_read(const KvReadParams& p, int head_dim, hipStream_t st);
+
+// ------------------------------------------------------------------ attention over a paged cache (attn_paged.hip)
+
+struct PagedAttnParams {
+  const uint16_t* q = nullptr;    // rows x n_heads x head_dim, stride ldq
+  uint16_t* out = nullptr;        // the same, stride ldo
+  int64_t rows = 0, ldq = 0, ldo = 0;
+  int n_heads = 0, group = 0;     // group: query heads a key/value head
+  int window = 0;                 // positions seen back, the own one included
+  float scale_log2 = 0.0f;        // score scale times log2(e)
+  PagedKv kv;
+  PagedBatch batch;
+};
+hipError_t launch_attn_paged(const PagedAttnParams& p, int head_dim, hipStream_t st);
+
+// ------------------------------------------------------------------ sampling (sample.hip)
+
+constexpr int64_t kSampleMaxVocab = 1 << 24;
+struct SampleParams {
+  const void* logits = nullptr;   // rows x n, stride ld, bf16 or f32
+  const float* u = nullptr;       // [rows]
+  const float* temperature = nullptr;  // [rows], or null: the value below
+  const int32_t* top_k = nullptr;
+  const float* top_p = nullptr;
+  const float* min_p = nullptr;
+  float temperature_all = 1.0f, top_p_all = 1.0f, min_p_all = 0.0f;
+  int top_k_all = 0;
+  int64_t rows = 0, n = 0, ld = 0;
+  int64_t* token = nullptr;       // [rows]
+  float* prob = nullptr;          // [rows] or null
+};
+hipError_t launch_sample(const SampleParams& p, bool bf16, hipStream_t st);
+
 }  // namespace w8a8

@@ -55,6 +55,28 @@ class StackDesc(ctypes.Structure):
                 ("lm_head_int8", LinearDesc), ("lm_head_bf16", P)]
 
 
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("head_dim", I64), ("rot_dim", I64), ("layout", INT), ("freq", P),
+                ("scale", ctypes.c_float)]
+
+
+class PagedKvDesc(ctypes.Structure):
+    _fields_ = [("n_pages", I64), ("page", I64), ("n_kv", I64), ("head_dim", I64), ("k", P),
+                ("v", P), ("sk", P), ("sv", P)]
+
+
+class PagedBatchDesc(ctypes.Structure):
+    _fields_ = [("n_seqs", I64), ("max_pages", I64), ("table", P), ("q_start", P),
+                ("ctx_len", P), ("max_q", I64)]
+
+
+class SampleDesc(ctypes.Structure):
+    _fields_ = [("temperature", P), ("temperature_all", ctypes.c_float),
+                ("top_k", P), ("top_k_all", ctypes.c_int32),
+                ("top_p", P), ("top_p_all", ctypes.c_float),
+                ("min_p", P), ("min_p_all", ctypes.c_float)]
+
+
 _SIGS = {
     "w8a8_packed_bytes": (SZ, [I64, I64]),
     "w8a8_packed_bf16_bytes": (SZ, [I64, I64]),
@@ -110,6 +132,20 @@ _SIGS = {
     "w8a8_attn_decode_workspace_bytes": (SZ, [I64]),
     "w8a8_attn_decode": (INT, [P, INT, I64, I64, P, P, P, P, I64, P, P, SZ, P]),
     "w8a8_attn_decode_bf16": (INT, [P, INT, I64, I64, P, P, I64, P, P, SZ, P]),
+    "w8a8_rope_frequencies": (INT, [I64, ctypes.c_double, INT, ctypes.c_double, ctypes.c_double,
+                                    P, P]),
+    "w8a8_rope": (INT, [ctypes.POINTER(RopeDesc), P, INT, I64, I64, I64, P, P, I64, P]),
+    "w8a8_kv_append": (INT, [P, I64, I64, I64, ctypes.POINTER(RopeDesc),
+                             ctypes.POINTER(PagedKvDesc), ctypes.POINTER(PagedBatchDesc), P, I64,
+                             P]),
+    "w8a8_kv_read": (INT, [ctypes.POINTER(PagedKvDesc), ctypes.POINTER(PagedBatchDesc), I64, P, P,
+                           P]),
+    "w8a8_attn_paged_workspace_bytes": (SZ, [I64, I64, I64, I64, I64, I64, I64]),
+    "w8a8_attn_paged": (INT, [P, I64, I64, I64, ctypes.POINTER(PagedKvDesc),
+                              ctypes.POINTER(PagedBatchDesc), I64, ctypes.c_float, P, I64, P, SZ,
+                              P]),
+    "w8a8_sample_workspace_bytes": (SZ, [I64, I64, INT]),
+    "w8a8_sample": (INT, [ctypes.POINTER(SampleDesc), P, INT, I64, I64, I64, P, P, P, P, SZ, P]),
     "w8a8_status_str": (ctypes.c_char_p, [INT]),
     "w8a8_last_error": (ctypes.c_char_p, []),
 }
@@ -768,6 +804,282 @@ def attn_decode(qkv, cache: KVCache, pos, window, n_heads=4, out=None, ws=None, 
                                            _ptr(cache.v), cache.t_max, _ptr(out), _ptr(ws),
                                            ws.numel(), _stream(stream)))
     return out
+
+
+# ---------------------------------------------------------------- rotary positions
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+
+class _on:
+    """The device of a call's tensors as the current one, and with a stream of
+    its own the call's new tensors in that stream's memory."""
+
+    def __init__(self, device, stream):
+        self.device, self.stream = device, stream
+
+    def __enter__(self):
+        self.old = torch.cuda.current_device()
+        if self.device.index != self.old:
+            torch.cuda.set_device(self.device)
+        self.ctx = None
+        if self.stream is not None:
+            if self.stream.device != self.device:
+                self.__exit__()
+                raise ValueError("the stream is not on the tensors' device")
+            self.ctx = torch.cuda.stream(self.stream)
+            self.ctx.__enter__()
+        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+        if self.device.index != self.old:
+            torch.cuda.set_device(self.old)
+
+
+def _need(t, name, dtype, device, shape=None):
+    """t as an argument: a contiguous GPU tensor of a type, on a device, of a shape."""
+    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype != dtype:
+        raise ValueError("%s must be a %s tensor on %s" % (name, dtype, device))
+    if not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError("%s must be contiguous%s" % (name, "" if shape is None else " of shape %s" % (tuple(shape),)))
+    return t
+
+
+def _row_stride(x, name):
+    """Elements from row to row of a [rows, heads, d] tensor whose rows are dense."""
+    if x.dim() != 3 or not x.is_cuda or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]):
+        raise ValueError("%s must be a GPU tensor [rows, heads, head_dim] with dense rows" % name)
+    return x.stride(0) if x.shape[0] > 1 else -(-x.shape[1] * x.shape[2] // 8) * 8
+
+
+@dataclass
+class Rope:
+    """Rotary positions of heads of head_dim: the first rot_dim elements in
+    pairs ("half": j and j + rot_dim / 2, "interleaved": 2 j and 2 j + 1), pair j
+    turned by freq[j] radians a position (float64 on the GPU); scale: the factor
+    on cosine and sine."""
+    head_dim: int
+    rot_dim: int
+    layout: str
+    freq: torch.Tensor
+    scale: float = 1.0
+
+    @classmethod
+    def make(cls, head_dim, rot_dim=None, theta=10000.0, layout="half", scaling="none", factor=1.0,
+             original=4096, device="cuda"):
+        rot_dim = head_dim if rot_dim is None else rot_dim
+        freq, scale = rope_frequencies(rot_dim, theta, scaling, factor, original)
+        return cls(head_dim, rot_dim, layout, torch.from_numpy(freq).to(device), scale)
+
+    def desc(self, device):
+        if self.layout not in ROPE_LAYOUTS:
+            raise ValueError("unknown rotary layout %r" % (self.layout,))
+        _need(self.freq, "freq", torch.float64, device, (self.rot_dim // 2,))
+        return RopeDesc(self.head_dim, self.rot_dim, ROPE_LAYOUTS[self.layout],
+                        self.freq.data_ptr(), self.scale)
+
+
+def rope_frequencies(rot_dim, theta=10000.0, scaling="none", factor=1.0, original=4096):
+    """(frequencies in radians a position as float64, factor on cosine and sine)."""
+    freq, scale = np.zeros(max(rot_dim // 2, 1), np.float64), np.zeros(1, np.float32)
+    if scaling not in ROPE_SCALINGS or lib().w8a8_rope_frequencies(
+            rot_dim, theta, ROPE_SCALINGS[scaling], factor, original, freq.ctypes.data_as(P),
+            scale.ctypes.data_as(P)) != 0:
+        raise ValueError("rope_frequencies: bad arguments")
+    return freq, float(scale[0])
+
+
+def rope(r: Rope, x, pos, out=None, stream=None):
+    """x: bf16 or f32 [rows, heads, head_dim], rows dense, at the positions pos
+    (int32 [rows]); out may be x (in place)."""
+    ldx = _row_stride(x, "x")
+    rows, heads, d = x.shape
+    if d != r.head_dim:
+        raise ValueError("x has heads of %d, the rotation of %d" % (d, r.head_dim))
+    _need(pos, "pos", torch.int32, x.device, (rows,))
+    with _on(x.device, stream) as st:
+        if out is None:
+            out = torch.empty((rows, heads, d), dtype=x.dtype, device=x.device)
+        elif out.dtype != x.dtype or out.device != x.device or out.shape != x.shape:
+            raise ValueError("out must be like x")
+        ldy = _row_stride(out, "out")
+        _check(lib().w8a8_rope(ctypes.byref(r.desc(x.device)), x.data_ptr(), _dt(x), rows, heads, ldx,
+                               pos.data_ptr(), out.data_ptr(), ldy, st))
+    return out
+
+
+# ---------------------------------------------------------------- paged key/value cache
+
+@dataclass
+class PagedKV:
+    """A key/value cache in pages that many sequences share: k, v
+    [n_pages, n_kv, page, head_dim], INT8 codes with scales sk, sv
+    [n_pages, n_kv, page], or bf16."""
+    k: torch.Tensor
+    v: torch.Tensor
+    sk: torch.Tensor | None = None
+    sv: torch.Tensor | None = None
+
+    @classmethod
+    def empty(cls, n_pages, page, n_kv=1, head_dim=HEAD_DIM, int8=True, device="cuda"):
+        shape = (n_pages, n_kv, page)
+        kv = [torch.zeros(shape + (head_dim,), dtype=torch.int8 if int8 else torch.bfloat16, device=device)
+              for _ in range(2)]
+        scales = [torch.zeros(shape, dtype=torch.float32, device=device) if int8 else None for _ in range(2)]
+        return cls(*kv, *scales)
+
+    def desc(self, device):
+        int8, shape = self.sk is not None, self.k.shape
+        dt = torch.int8 if int8 else torch.bfloat16
+        if len(shape) != 4:
+            raise ValueError("k must be [n_pages, n_kv, page, head_dim]")
+        _need(self.k, "k", dt, device)
+        _need(self.v, "v", dt, device, shape)
+        if int8 or self.sv is not None:
+            _need(self.sk, "sk", torch.float32, device, shape[:3])
+            _need(self.sv, "sv", torch.float32, device, shape[:3])
+        return PagedKvDesc(shape[0], shape[2], shape[1], shape[3], self.k.data_ptr(), self.v.data_ptr(),
+                           self.sk.data_ptr() if int8 else None, self.sv.data_ptr() if int8 else None)
+
+
+@dataclass
+class PagedBatch:
+    """The sequences of a call, int32 on the GPU: table [n_seqs, max_pages] (an
+    entry outside the cache: a page not held), q_start [n_seqs + 1] (the new
+    tokens' rows), ctx_len [n_seqs] (positions, the new ones included); max_q: no
+    sequence has more new tokens."""
+    table: torch.Tensor
+    q_start: torch.Tensor
+    ctx_len: torch.Tensor
+    max_q: int
+
+    def desc(self, device):
+        n = self.ctx_len.shape[0]
+        _need(self.table, "table", torch.int32, device)
+        _need(self.ctx_len, "ctx_len", torch.int32, device, (n,))
+        _need(self.q_start, "q_start", torch.int32, device, (n + 1,))
+        if self.table.dim() != 2 or self.table.shape[0] != n:
+            raise ValueError("table must be [n_seqs, max_pages]")
+        return PagedBatchDesc(n, self.table.shape[1], self.table.data_ptr(), self.q_start.data_ptr(),
+                              self.ctx_len.data_ptr(), self.max_q)
+
+
+def _bf16_rows(x, name):
+    if not isinstance(x, torch.Tensor) or x.dtype != torch.bfloat16 or not x.is_cuda:
+        raise ValueError("%s must be a bf16 GPU tensor" % name)
+
+
+def kv_append(qkv, cache: PagedKV, batch: PagedBatch, n_heads, rope: Rope | None = None, out=None, stream=None):
+    """Stores the new tokens' keys and values (from rows of a fused QKV
+    projection, bf16 [rows, (n_heads + 2 n_kv) * head_dim], rows dense) in the
+    cache, rotated by rope; returns the rotated queries, bf16
+    [rows, n_heads, head_dim]."""
+    _bf16_rows(qkv, "qkv")
+    kv = cache.desc(qkv.device)
+    rows, width = qkv.shape
+    if qkv.stride(1) != 1 or width != (n_heads + 2 * kv.n_kv) * kv.head_dim:
+        raise ValueError("qkv must have dense rows of (n_heads + 2 n_kv) * head_dim")
+    with _on(qkv.device, stream) as st:
+        if out is None:
+            out = torch.empty((rows, n_heads, kv.head_dim), dtype=torch.bfloat16, device=qkv.device)
+        elif out.dtype != torch.bfloat16 or out.device != qkv.device or tuple(out.shape) != (rows, n_heads, kv.head_dim):
+            raise ValueError("out must be bf16 [rows, n_heads, head_dim] on qkv's device")
+        r = None if rope is None else ctypes.byref(rope.desc(qkv.device))
+        ldq = _row_stride(out, "out")
+        ld = qkv.stride(0) if rows > 1 else ldq if qkv.data_ptr() == out.data_ptr() and ldq >= width else width
+        if rows == 1 and qkv.data_ptr() == out.data_ptr():
+            ldq = ld
+        _check(lib().w8a8_kv_append(qkv.data_ptr(), rows, ld, n_heads, r, ctypes.byref(kv),
+                                    ctypes.byref(batch.desc(qkv.device)), out.data_ptr(), ldq, st))
+    return out
+
+
+def kv_read(cache: PagedKV, batch: PagedBatch, rows, k=None, v=None, stream=None):
+    """The cached rows of the batch's new tokens (rows of them, padding
+    included) as bf16 (k, v) [rows, n_kv, head_dim]."""
+    device = cache.k.device
+    kv = cache.desc(device)
+    shape = (rows, kv.n_kv, kv.head_dim)
+    with _on(device, stream) as st:
+        k, v = (torch.empty(shape, dtype=torch.bfloat16, device=device) if t is None
+                else _need(t, name, torch.bfloat16, device, shape) for t, name in ((k, "k"), (v, "v")))
+        _check(lib().w8a8_kv_read(ctypes.byref(kv), ctypes.byref(batch.desc(device)), rows, k.data_ptr(),
+                                  v.data_ptr(), st))
+    return k, v
+
+
+def attn_paged_workspace_bytes(rows, n_heads, n_kv, head_dim, n_seqs, max_q, ctx_max):
+    return lib().w8a8_attn_paged_workspace_bytes(rows, n_heads, n_kv, head_dim, n_seqs, max_q, ctx_max)
+
+
+def attn_paged(q, cache: PagedKV, batch: PagedBatch, window=None, scale=None, out=None, ws=None, stream=None):
+    """Attention of the new tokens (q: bf16 [rows, n_heads, head_dim], rows
+    dense, e.g. from kv_append) over the cache, which holds their rows; window:
+    positions seen back, the own one included (None: all); scale: of the scores
+    (None: head_dim ** -0.5)."""
+    _bf16_rows(q, "q")
+    ldq = _row_stride(q, "q")
+    rows, heads, d = q.shape
+    kv, b = cache.desc(q.device), batch.desc(q.device)
+    if d != kv.head_dim:
+        raise ValueError("q has heads of %d, the cache of %d" % (d, kv.head_dim))
+    with _on(q.device, stream) as st:
+        if out is None:
+            out = torch.empty((rows, heads, d), dtype=torch.bfloat16, device=q.device)
+        elif out.dtype != torch.bfloat16 or out.device != q.device or out.shape != q.shape:
+            raise ValueError("out must be like q")
+        ldo = _row_stride(out, "out")
+        if ws is None:
+            ws = _empty(attn_paged_workspace_bytes(rows, heads, kv.n_kv, d, b.n_seqs, b.max_q,
+                                                   b.max_pages * kv.page), q.device)
+        elif ws.device != q.device:
+            raise ValueError("ws must be on q's device")
+        _check(lib().w8a8_attn_paged(q.data_ptr(), rows, ldq, heads, ctypes.byref(kv), ctypes.byref(b),
+                                     2 ** 31 - 1 if window is None else window,
+                                     d ** -0.5 if scale is None else scale, out.data_ptr(), ldo,
+                                     ws.data_ptr(), ws.numel() * ws.element_size(), st))
+    return out
+
+
+# ---------------------------------------------------------------- sampling
+
+def sample_workspace_bytes(rows, n, dtype):
+    return lib().w8a8_sample_workspace_bytes(rows, n, {torch.float32: F32, torch.bfloat16: BF16}[dtype])
+
+
+def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, prob=None, ws=None, stream=None):
+    """One token for each row of logits (bf16 or f32 [rows, n], unit column
+    stride) from the uniform numbers u (float32 [rows]): (tokens int64, the
+    probability each was drawn with).  temperature, top_p, min_p: a number or
+    float32 [rows]; top_k: a number or int32 [rows]; None: off."""
+    if not logits.is_cuda or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be a GPU tensor [rows, n] with unit column stride")
+    rows, n = logits.shape
+    device, dt = logits.device, _dt(logits)
+    _need(u, "u", torch.float32, device, (rows,))
+    d = SampleDesc(None, 1.0, None, 0, None, 1.0, None, 0.0)
+    for name, x, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if isinstance(x, torch.Tensor):
+            setattr(d, name, _need(x, name, dtype, device, (rows,)).data_ptr())
+        elif x is not None:
+            setattr(d, name + "_all", x)
+    with _on(device, stream) as st:
+        out = torch.empty(rows, dtype=torch.int64, device=device) if out is None \
+            else _need(out, "out", torch.int64, device, (rows,))
+        prob = torch.empty(rows, dtype=torch.float32, device=device) if prob is None \
+            else _need(prob, "prob", torch.float32, device, (rows,))
+        if ws is None:
+            ws = _empty(lib().w8a8_sample_workspace_bytes(rows, n, dt), device)
+        elif ws.device != device:
+            raise ValueError("ws must be on the logits' device")
+        _check(lib().w8a8_sample(ctypes.byref(d), logits.data_ptr(), dt, rows, n,
+                                 max(n, logits.stride(0) if rows > 1 else n), u.data_ptr(), out.data_ptr(),
+                                 prob.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), st))
+    return out, prob
 
 
 def frag_to_rowmajor(packed: np.ndarray, rows: int, k: int) -> np.ndarray:
