@@ -645,7 +645,8 @@ typedef struct {
    are never drawn; of +inf ones each has weight 1 and all others 0.  A row with
    nothing to draw gives token -1 (and prob 0).
    u: DEVICE float[rows]; token: DEVICE int64[rows]; prob: DEVICE float[rows] or
-   NULL, w_token / sum_{kept} w.  n <= 2^24 (EUNSUPPORTED otherwise).
+   NULL, w_token / sum_{kept} w.  n <= 2^24, rows <= 65535 (EUNSUPPORTED
+   otherwise).
    ws: w8a8_sample_workspace_bytes(rows, n, dtype) bytes (may be NULL when 0). */
 size_t w8a8_sample_workspace_bytes(int64_t rows, int64_t n, w8a8_dtype dtype);
 w8a8_status w8a8_sample(const w8a8_sample_desc* desc, const void* logits, w8a8_dtype dtype,

@@ -2282,7 +2282,10 @@ w8a8_status w8a8_attn_paged(const void* q, int64_t rows, int64_t ldq, int64_t n_
   return hip_check(launch_attn_paged(p, (int)kv->head_dim, S(stream)), "attn_paged");
 }
 
-size_t w8a8_sample_workspace_bytes(int64_t rows, int64_t n, w8a8_dtype dtype) { return 0; }
+size_t w8a8_sample_workspace_bytes(int64_t rows, int64_t n, w8a8_dtype dtype) {
+  if (rows < 1 || rows > kSampleMaxRows || n < 1 || n > kSampleMaxVocab) return 0;
+  return align256(sample_ws_bytes(rows, n, dtype == W8A8_BF16));
+}
 
 w8a8_status w8a8_sample(const w8a8_sample_desc* desc, const void* logits, w8a8_dtype dtype,
                         int64_t rows, int64_t n, int64_t ld, const float* u, int64_t* token,
@@ -2298,7 +2301,7 @@ w8a8_status w8a8_sample(const w8a8_sample_desc* desc, const void* logits, w8a8_d
   REQUIRE(u && ((uintptr_t)u & 3) == 0, W8A8_EINVAL, "u is NULL or not 4-byte aligned");
   REQUIRE(token && ((uintptr_t)token & 7) == 0, W8A8_EINVAL, "token is NULL or not 8-byte aligned");
   REQUIRE(rows >= 1 && n >= 1, W8A8_EINVAL, "rows or n < 1");
-  REQUIRE(rows <= (1 << 20) && n <= kSampleMaxVocab, W8A8_EUNSUPPORTED, "more than 2^20 rows or 2^24 logits a row");
+  REQUIRE(rows <= kSampleMaxRows && n <= kSampleMaxVocab, W8A8_EUNSUPPORTED, "more than 65535 rows or 2^24 logits a row");
   REQUIRE(ld >= n && ld <= ((int64_t)1 << 32), W8A8_EINVAL, "ld is below n or above 2^32");
   REQUIRE(!std::isnan(desc->temperature_all) && !std::isnan(desc->top_p_all) && !std::isnan(desc->min_p_all),
           W8A8_EINVAL, "temperature_all, top_p_all or min_p_all is NaN");
@@ -2318,7 +2321,11 @@ w8a8_status w8a8_sample(const w8a8_sample_desc* desc, const void* logits, w8a8_d
   p.ld = ld;
   p.token = token;
   p.prob = prob;
-  return hip_check(launch_sample(p, dtype == W8A8_BF16, S(stream)), "sample");
+  if (const size_t need = w8a8_sample_workspace_bytes(rows, n, dtype)) {
+    CHECK_PTR(ws);
+    REQUIRE(ws_bytes >= need, W8A8_EWORKSPACE, "workspace too small");
+  }
+  return hip_check(launch_sample(p, dtype == W8A8_BF16, ws, S(stream)), "sample");
 }
 
 }  // extern "C"

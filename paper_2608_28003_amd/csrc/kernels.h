@@ -366,7 +366,7 @@ hipError_t launch_attn_paged(const PagedAttnParams& p, int head_dim, hipStream_t
 
 // ------------------------------------------------------------------ sampling (sample.hip)
 
-constexpr int64_t kSampleMaxVocab = 1 << 24;
+constexpr int64_t kSampleMaxVocab = 1 << 24, kSampleMaxRows = 65535;
 struct SampleParams {
   const void* logits = nullptr;   // rows x n, stride ld, bf16 or f32
   const float* u = nullptr;       // [rows]
@@ -380,6 +380,7 @@ struct SampleParams {
   int64_t* token = nullptr;       // [rows]
   float* prob = nullptr;          // [rows] or null
 };
-hipError_t launch_sample(const SampleParams& p, bool bf16, hipStream_t st);
+size_t sample_ws_bytes(int64_t rows, int64_t n, bool bf16);
+hipError_t launch_sample(const SampleParams& p, bool bf16, void* ws, hipStream_t st);
 
 }  // namespace w8a8

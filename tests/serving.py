@@ -175,7 +175,7 @@ def draw(l, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     else:
         with np.errstate(invalid="ignore", over="ignore"):
             w = np.where(l[order] == top, 1.0, np.exp((l[order] - top) / np.float64(temperature)))
-        w = np.where(l[order] == -np.inf, 0.0, w)
+        w = np.where((l[order] == -np.inf) | ((top == np.inf) & (l[order] != top)), 0.0, w)
         if 0 < top_k < len(w):
             w = w[:top_k]
         if top_p < 1:

@@ -174,3 +174,29 @@ def test_binding_refusals():
         w8a8.sample(l.half(), u)
     with pytest.raises(w8a8.W8A8Error):
         w8a8.sample(l, u, temperature=math.nan)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_prefixes_that_end_far_below_the_largest_logit(dt):
+    """More than a thousand bf16 values apart, across 0, with and without the
+    other filters; and temperatures that make all weights alike or all but one 0."""
+    g = serving.gen(14)
+    l = torch.cat([torch.randn((5, 20000), generator=g) * 1e-3, torch.full((5, 4), 8.0)], 1).to(dt)
+    check(l, uniform(5), k=torch.tensor([3, 5, 5000, 11000, 20003], dtype=torch.int32))
+    check(l, uniform(5), p=torch.tensor([0.2, 0.4, 0.7, 0.99, 0.999999]))
+    check(l, uniform(5), m=torch.tensor([1e-7, 1e-3, 3.3e-4, 3.4e-4, 0.5]))
+    check(l, uniform(5), k=15000, p=0.9, m=3.36e-4)
+    for t in (1e30, math.inf, 1e-30, 2.0 ** -149):
+        check(l, uniform(5), t=t)
+        check(l, uniform(5), t=t, k=12000, p=0.5)
+    l[:, 7] = math.inf
+    check(l, uniform(5), t=math.inf)
+
+
+def test_workspace_refusal():
+    l, u = torch.zeros((2, 100), dtype=torch.bfloat16, device=DEV), torch.zeros(2, device=DEV)
+    need = w8a8.sample_workspace_bytes(2, 100, torch.bfloat16)
+    assert need > 0
+    with pytest.raises(w8a8.W8A8Error) as e:
+        w8a8.sample(l, u, ws=torch.empty(need - 1, dtype=torch.uint8, device=DEV))
+    assert e.value.status == w8a8.EWORKSPACE
