@@ -608,15 +608,15 @@ w8a8_status w8a8_kv_read(const w8a8_paged_kv* kv, const w8a8_paged_batch* batch,
      out = sum_j softmax_j(scale * q . k_j) v_j,
    zeros where there is none.  q, out: bf16 rows x n_heads x head_dim, strides
    ldq and ldo (multiples of 8).  n_heads: a multiple of n_kv.  window >= 1
-   (e.g. INT32_MAX for none), scale finite (1 / sqrt(head_dim) as a rule).  Sums
+   (2^30 and more: none), scale finite (1 / sqrt(head_dim) as a rule).  Sums
    and softmax statistics are binary32.  Cached rows past ctx_len, before every
    new token's window and in pages that are not held are never used.
-   ws: w8a8_attn_paged_workspace_bytes(...) bytes (may be NULL when that is 0);
-   ctx_max: the longest context that ctx_len may hold (max_pages * page at most
-   is used). */
+   ws: w8a8_attn_paged_workspace_bytes(...) bytes of the same sizes, with ctx_max =
+   max_pages * page, the positions that the tables can hold (may be NULL when
+   that is 0).  Calls that share a workspace must not overlap in time. */
 size_t w8a8_attn_paged_workspace_bytes(int64_t rows, int64_t n_heads, int64_t n_kv,
                                        int64_t head_dim, int64_t n_seqs, int64_t max_q,
-                                       int64_t ctx_max);
+                                       int64_t window, int64_t ctx_max);
 w8a8_status w8a8_attn_paged(const void* q, int64_t rows, int64_t ldq, int64_t n_heads,
                             const w8a8_paged_kv* kv, const w8a8_paged_batch* batch,
                             int64_t window, float scale, void* out, int64_t ldo, void* ws,

@@ -2251,8 +2251,17 @@ w8a8_status w8a8_kv_read(const w8a8_paged_kv* kv, const w8a8_paged_batch* batch,
 
 size_t w8a8_attn_paged_workspace_bytes(int64_t rows, int64_t n_heads, int64_t n_kv,
                                        int64_t head_dim, int64_t n_seqs, int64_t max_q,
-                                       int64_t ctx_max) {
-  return 0;
+                                       int64_t window, int64_t ctx_max) {
+  if (rows < 1 || n_kv < 1 || n_heads < n_kv || n_heads % n_kv || n_seqs < 1 || max_q < 1 || window < 1 || ctx_max < 1) return 0;
+  if (rows > (1 << 25) || n_heads > 4096 || n_seqs > (1 << 20) || ctx_max > (1 << 30)) return 0;
+  PagedAttnParams p;
+  p.rows = rows;
+  p.group = (int)(n_heads / n_kv);
+  p.window = (int)std::min<int64_t>(window, 1 << 30);
+  p.kv.n_kv = (int)n_kv;
+  p.batch.n_seqs = (int)n_seqs;
+  attn_paged_plan(&p, std::min(max_q, rows), ctx_max);
+  return align256(attn_paged_ws_bytes(p, (int)head_dim));
 }
 
 w8a8_status w8a8_attn_paged(const void* q, int64_t rows, int64_t ldq, int64_t n_heads,
@@ -2279,7 +2288,12 @@ w8a8_status w8a8_attn_paged(const void* q, int64_t rows, int64_t ldq, int64_t n_
   p.group = (int)(n_heads / kv->n_kv);
   p.window = (int)std::min<int64_t>(window, 1 << 30);  // no position reaches it
   p.scale_log2 = scale * 1.44269504088896341f;
-  return hip_check(launch_attn_paged(p, (int)kv->head_dim, S(stream)), "attn_paged");
+  attn_paged_plan(&p, std::min(batch->max_q, rows), batch->max_pages * kv->page);
+  if (const size_t need = attn_paged_ws_bytes(p, (int)kv->head_dim)) {
+    CHECK_PTR(ws);
+    REQUIRE(ws_bytes >= need, W8A8_EWORKSPACE, "workspace too small");
+  }
+  return hip_check(launch_attn_paged(p, (int)kv->head_dim, ws, S(stream)), "attn_paged");
 }
 
 size_t w8a8_sample_workspace_bytes(int64_t rows, int64_t n, w8a8_dtype dtype) {

@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kStep = 32;          // keys a wave takes at a time
 constexpr int kPass = 4 * kStep;   // ... and a workgroup
+constexpr int kRows = 16;          // rows of the row-tile kernel
 
 // INT8 code e of a word (exact in bf16)
 __device__ __forceinline__ float byte_f(uint32_t w, int e) {
@@ -33,69 +34,130 @@ __device__ __forceinline__ int pair_hi(float lo, float hi) {
   return (int)__builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
 }
 
-// A tile of BM rows of one sequence.  Sequence s has slots floor(q_start[s] *
-// group / BM) + s and up, one for each of its tiles at least: a workgroup finds
-// its sequence without a prefix sum, and slots between the sequences are empty.
-struct Tile {
-  int seq, q0, q_len, row0;
+// The new tokens of sequence s, false where it has none (or its arrays are not
+// what they should be: rows outside the call, more tokens than the workspace is
+// for; those rows are not touched).
+struct Seq {
+  int q0, q_len;
   int first;  // position of the first new token
 };
-template <int BM>
-__device__ __forceinline__ bool find_tile(const PagedAttnParams& p, int64_t slot, Tile* t) {
-  int count = 0;
-  for (int base = 0; base < p.batch.n_seqs; base += kWave) {
-    const int s = base + lane_id();
-    const uint64_t m = __ballot(s < p.batch.n_seqs && (int64_t)p.batch.q_start[min(s, p.batch.n_seqs)] * p.group / BM + s <= slot);
-    count += __popcll(m);
-    if (m != ~0ull) break;
-  }
-  if (count == 0) return false;
-  const int s = count - 1, q0 = p.batch.q_start[s], q1 = p.batch.q_start[s + 1];
-  if (q0 < 0 || q1 > p.rows || q1 <= q0) return false;
-  const int64_t row0 = (slot - (int64_t)q0 * p.group / BM - s) * BM;
-  if (row0 < 0 || row0 >= (int64_t)(q1 - q0) * p.group) return false;
-  t->seq = s;
+__device__ __forceinline__ bool seq_of(const PagedAttnParams& p, int s, Seq* t) {
+  const int q0 = p.batch.q_start[s], q1 = p.batch.q_start[s + 1];
+  if (q0 < 0 || q1 > p.rows || q1 <= q0 || q1 - q0 > p.max_q) return false;
   t->q0 = q0;
   t->q_len = q1 - q0;
   t->first = max(p.batch.ctx_len[s], 0) - t->q_len;
-  t->row0 = (int)row0;
   return true;
+}
+
+// Keys [lo, hi) that rows row0 .. row1 of a sequence attend, lo in [0, hi]: no
+// position below leaves 32 bits (first positions from -2^25, windows and tables up
+// to 2^30).  Pieces of `piece` keys from lo rounded down to a step; one at least.
+struct Keys {
+  int lo, hi, begin, pieces;
+};
+__device__ __forceinline__ Keys keys_of(const PagedAttnParams& p, const Seq& t, int row0, int row1, int piece) {
+  Keys k;
+  k.hi = min(t.first + row1 / p.group + 1, p.batch.max_pages << p.kv.page_log2);
+  k.lo = min(max(0, t.first + row0 / p.group + 1 - p.window), max(k.hi, 0));
+  k.begin = k.lo & ~(kStep - 1);
+  k.pieces = max((k.hi - k.begin + piece - 1) / piece, 1);
+  return k;
 }
 
 }  // namespace
 
-// Sixteen rows a workgroup.  Each of its four waves walks every fourth group of
-// 32 keys, straight from memory: a lane's pieces of a key row are what lies
-// together in memory (any assignment of the dimensions to the product's K
-// positions serves), and its 16 bytes of a value row are one output dimension
-// of sixteen products.  The weights go in as two bf16 values (16 significant
-// bits).
+// Sequences of at most 16 rows, one a workgroup, and for long contexts a piece of
+// its keys.  Each of the four waves walks every fourth group of 32 keys, straight
+// from memory: a lane's pieces of a key row are what lies together in memory (any
+// assignment of the dimensions to the product's K positions serves), and its 16
+// bytes of a value row are one output dimension of sixteen products.  The weights
+// go in as two bf16 values (16 significant bits).  The next group's keys and
+// values are loaded as soon as the registers of this one's are free.  Rows of a
+// held page are read whatever they hold; what no row attends is masked out of the
+// scores, and zeroed in bf16 values (a weight of 0 times NaN).
 template <int D, bool I8>
-__global__ __launch_bounds__(256) void attn_paged_kernel(PagedAttnParams p) {
+__global__ __launch_bounds__(256, I8 ? 2 : 1) void attn_rows_kernel(PagedAttnParams p) {
   constexpr int KI = I8 ? D / 64 : D / 32;  // 16-byte pieces of a lane's quarter of a key row
   constexpr int E = D / 16;                 // dimensions of a lane's part of a value row
   constexpr int VW = I8 ? E / 4 : E / 2;    // ... in words
   constexpr int ROWB = I8 ? D : 2 * D;
   constexpr int LD = D + 4;
-  __shared__ __attribute__((aligned(16))) float ored[2][16][LD];
-  __shared__ float om[4][16], ol[4][16];
+  __shared__ __attribute__((aligned(16))) float ored[2][kRows][LD];
+  __shared__ float om[4][kRows], ol[4][kRows];
 
-  Tile tl;
-  if (!find_tile<16>(p, blockIdx.x, &tl)) return;  // whole workgroup
-  const int j = blockIdx.y;
-  const int tid = threadIdx.x, w = tid >> 6, l = lane_id(), n = l & 15, g = l >> 4;
-  const int first = tl.first, rows = tl.q_len * p.group, row = tl.row0 + n;
-  const int pos = row < rows ? first + row / p.group : -1;
+  Seq tl;
+  const int seq = blockIdx.x, j = blockIdx.y, split = blockIdx.z;
+  if (!seq_of(p, seq, &tl)) return;  // whole workgroup
+  const int rows = tl.q_len * p.group;
+  if (rows > p.max_rows) return;
+  const Keys ks = keys_of(p, tl, 0, rows - 1, p.piece);
+  if (split >= ks.pieces) return;
+  const int lo = ks.lo, hi = min(ks.hi, ks.begin + (split + 1) * p.piece);
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = lane_id(), n = l & 15, g = l >> 4;
+  const int pos = n < rows ? tl.first + n / p.group : -1;
   const int from = pos < 0 ? 0 : max(0, pos + 1 - p.window);
-  const int hi = min(first + min(rows - 1, tl.row0 + 15) / p.group + 1, p.batch.max_pages << p.kv.page_log2);  // exclusive
-  // in [0, hi], so that no position below leaves 32 bits: a first position down to
-  // -2^25 and a window up to 2^30 (the launcher's bound) are within them, too
-  const int lo = min(max(0, first + tl.row0 / p.group + 1 - p.window), max(hi, 0));
-  const int32_t* table = p.batch.table + (int64_t)tl.seq * p.batch.max_pages;
+  const int32_t* table = p.batch.table + (int64_t)seq * p.batch.max_pages;
+  const int page_mask = (1 << p.kv.page_log2) - 1;
 
+  uint4 kc[2][KI];       // key row 16 t + n, bytes 64 i + 16 g .. + 15
+  uint32_t vc[8][VW];    // value row 16 t + 4 g + i (at 4 t + i), dimensions E n .. + E - 1
+  float4 sk[2], sv[2];   // INT8: scales of rows 16 t + 4 g .. + 3
+  bool held[2];
+  int64_t at[2];
+  // the pages of two 16-key tiles (wave-uniform: scalar loads)
+  auto locate = [&](int r0) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int k0 = r0 + 16 * t;
+      const int page = k0 < hi ? table[k0 >> p.kv.page_log2] : -1;
+      held[t] = page >= 0 && page < p.kv.n_pages;
+      at[t] = held[t] ? ((((int64_t)page * p.kv.n_kv + j) << p.kv.page_log2) + (k0 & page_mask)) : 0;
+    }
+  };
+  auto load_k = [&]() {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int8_t* kp = reinterpret_cast<const int8_t*>(p.kv.k) + (at[t] + n) * ROWB + 16 * g;
+#pragma unroll
+      for (int i = 0; i < KI; ++i) kc[t][i] = *reinterpret_cast<const uint4*>(kp + 64 * i);
+      if constexpr (I8) sk[t] = *reinterpret_cast<const float4*>(p.kv.sk + at[t] + 4 * g);
+    }
+  };
+  auto load_v = [&]() {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int8_t* vp = reinterpret_cast<const int8_t*>(p.kv.v) + (at[t] + 4 * g) * ROWB + 4 * VW * n;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (VW >= 4) {
+#pragma unroll
+          for (int c = 0; c < VW; c += 4) {
+            const uint4 x = *reinterpret_cast<const uint4*>(vp + i * ROWB + 4 * c);
+            vc[4 * t + i][c] = x.x;
+            vc[4 * t + i][c + 1] = x.y;
+            vc[4 * t + i][c + 2] = x.z;
+            vc[4 * t + i][c + 3] = x.w;
+          }
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(vp + i * ROWB);
+          vc[4 * t + i][0] = x.x;
+          vc[4 * t + i][1] = x.y;
+        }
+      }
+      if constexpr (I8) sv[t] = *reinterpret_cast<const float4*>(p.kv.sv + at[t] + 4 * g);
+    }
+  };
+
+  int r0 = ks.begin + split * p.piece + kStep * w;
+  if (r0 < hi) {
+    locate(r0);
+    load_k();
+    load_v();
+  }
   v4i q[D / 32];
   {
-    const int r = min(row, rows - 1);
+    const int r = min(n, rows - 1);
     const uint16_t* src = p.q + (int64_t)(tl.q0 + r / p.group) * p.ldq + (int64_t)(j * p.group + r % p.group) * D;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
@@ -109,51 +171,51 @@ __global__ __launch_bounds__(256) void attn_paged_kernel(PagedAttnParams p) {
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = v4f{0.f, 0.f, 0.f, 0.f};
 
-  for (int r0 = (lo & ~(kStep - 1)) + kStep * w; r0 < hi; r0 += kPass) {
-    float sc[8], vs[8];
-    uint32_t vc[8][VW];
+  for (; r0 < hi; r0 += kPass) {
+    const bool more = r0 + kPass < hi;
     // ---- scores of two 16-key tiles
+    float sc[8], vs[8];
+    const bool h0 = held[0], h1 = held[1];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int k0 = r0 + 16 * t;
-      const int page = k0 < hi ? table[k0 >> p.kv.page_log2] : -1;
-      const bool held = page >= 0 && page < p.kv.n_pages;
-      const int64_t at = held ? ((((int64_t)page * p.kv.n_kv + j) << p.kv.page_log2) + (k0 & ((1 << p.kv.page_log2) - 1))) : 0;
-      const int8_t* kp = reinterpret_cast<const int8_t*>(p.kv.k) + (at + n) * ROWB + 16 * g;
-      uint4 kc[KI];
-      const bool in = held && k0 + n >= lo && k0 + n < hi;  // other rows are not read
-#pragma unroll
-      for (int i = 0; i < KI; ++i)
-        kc[i] = in ? *reinterpret_cast<const uint4*>(kp + 64 * i) : make_uint4(0, 0, 0, 0);
       v4f s = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
         v4i kf;
         if constexpr (I8) {
-          const uint4 u = kc[c >> 1];
+          const uint4 u = kc[t][c >> 1];
           const uint32_t a = c & 1 ? u.z : u.x, b = c & 1 ? u.w : u.y;
           kf = v4i{pair_hi(byte_f(a, 0), byte_f(a, 1)), pair_hi(byte_f(a, 2), byte_f(a, 3)),
                    pair_hi(byte_f(b, 0), byte_f(b, 1)), pair_hi(byte_f(b, 2), byte_f(b, 3))};
         } else {
-          kf = __builtin_bit_cast(v4i, kc[c]);
+          kf = __builtin_bit_cast(v4i, kc[t][c]);
         }
         s = mma_bf16(kf, q[c], s);
       }
+      const float ks4[4] = {I8 ? sk[t].x : 1.f, I8 ? sk[t].y : 1.f, I8 ? sk[t].z : 1.f, I8 ? sk[t].w : 1.f};
+      const float vs4[4] = {I8 ? sv[t].x : 1.f, I8 ? sv[t].y : 1.f, I8 ? sv[t].z : 1.f, I8 ? sv[t].w : 1.f};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int key = k0 + 4 * g + i;
-        const bool live = held && key >= lo && key < hi;
-        float x = s[i] * p.scale_log2;
-        vs[4 * t + i] = 1.0f;
-        if constexpr (I8) {
-          x *= live ? p.kv.sk[at + 4 * g + i] : 0.0f;
-          vs[4 * t + i] = live ? p.kv.sv[at + 4 * g + i] : 0.0f;
-        }
-        sc[4 * t + i] = held && key >= from && key <= pos ? x : -INFINITY;
-        const uint32_t* vp = reinterpret_cast<const uint32_t*>(reinterpret_cast<const int8_t*>(p.kv.v) + (at + 4 * g + i) * ROWB) + VW * n;
-#pragma unroll
-        for (int c = 0; c < VW; ++c) vc[4 * t + i][c] = live ? vp[c] : 0u;
+        const int key = r0 + 16 * t + 4 * g + i;
+        const float x = s[i] * (I8 ? ks4[i] * p.scale_log2 : p.scale_log2);
+        sc[4 * t + i] = (t ? h1 : h0) && key >= from && key <= pos && key < hi ? x : -INFINITY;
+        vs[4 * t + i] = vs4[i];
       }
+    }
+    if constexpr (!I8) {
+      if (!(h0 && h1 && r0 >= lo && r0 + kStep <= hi)) {  // wave-uniform
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int key = r0 + 16 * (i >> 2) + 4 * g + (i & 3);
+          const bool live = (i < 4 ? h0 : h1) && key >= lo && key < hi;
+#pragma unroll
+          for (int c = 0; c < VW; ++c) vc[i][c] = live ? vc[i][c] : 0u;
+        }
+      }
+    }
+    if (more) {
+      locate(r0 + kPass);
+      load_k();
     }
     // ---- running softmax
     float mx = run_m;
@@ -166,8 +228,10 @@ __global__ __launch_bounds__(256) void attn_paged_kernel(PagedAttnParams p) {
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      sc[i] = __builtin_amdgcn_exp2f(sc[i] - ref);
+      const float x = sc[i];
+      sc[i] = __builtin_amdgcn_exp2f(x - ref);
       sum += sc[i];
+      if constexpr (I8) sc[i] = x == -INFINITY ? 0.0f : sc[i] * vs[i];  // a scale no row attends may be NaN
     }
     sum += lane_xor<16>(sum);
     sum += lane_xor<32>(sum);
@@ -180,9 +244,8 @@ __global__ __launch_bounds__(256) void attn_paged_kernel(PagedAttnParams p) {
       float a[2], b[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const float wt = I8 ? (sc[i + k] == 0.0f ? 0.0f : sc[i + k] * vs[i + k]) : sc[i + k];
-        a[k] = bf16_bits_to_float(float_to_bf16_bits(wt));
-        b[k] = bf16_bits_to_float(float_to_bf16_bits(wt - a[k]));
+        a[k] = bf16_bits_to_float(float_to_bf16_bits(sc[i + k]));
+        b[k] = bf16_bits_to_float(float_to_bf16_bits(sc[i + k] - a[k]));
       }
       hi2[i >> 1] = pair_hi(a[0], a[1]);
       lo2[i >> 1] = pair_hi(b[0], b[1]);
@@ -199,6 +262,7 @@ __global__ __launch_bounds__(256) void attn_paged_kernel(PagedAttnParams p) {
       }
       acc[e] = mma_bf16(vf, lo2, mma_bf16(vf, hi2, acc[e] * corr));
     }
+    if (more) load_v();
   }
 
   // ---- the four waves
@@ -235,35 +299,498 @@ __global__ __launch_bounds__(256) void attn_paged_kernel(PagedAttnParams p) {
       }
   }
   __syncthreads();
-  // ---- 16 rows of D: thread tid has eight dimensions of a row
-  for (int i = tid; i < 16 * D / 8; i += 256) {
-    const int rr = i / (D / 8), d0 = 8 * (i % (D / 8)), r = tl.row0 + rr;
-    if (r >= rows) break;
-    const float mr = fmaxf(fmaxf(om[0][rr], om[1][rr]), fmaxf(om[2][rr], om[3][rr]));
+  // ---- rows of D: thread tid has eight dimensions of a row
+  for (int i = tid; i < rows * D / 8; i += 256) {
+    const int r = i / (D / 8), d0 = 8 * (i % (D / 8));
+    const float mr = fmaxf(fmaxf(om[0][r], om[1][r]), fmaxf(om[2][r], om[3][r]));
     const float rref = mr == -INFINITY ? 0.0f : mr;
-    float den = 0.0f;
+    float den = 0.0f, x[8];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) den += ol[k][rr] * __builtin_amdgcn_exp2f(om[k][rr] - rref);
-    uint32_t o[4];
+    for (int k = 0; k < 4; ++k) den += ol[k][r] * __builtin_amdgcn_exp2f(om[k][r] - rref);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float x = ored[0][rr][d0 + 2 * k] + ored[1][rr][d0 + 2 * k];
-      const float y = ored[0][rr][d0 + 2 * k + 1] + ored[1][rr][d0 + 2 * k + 1];
-      o[k] = (uint32_t)float_to_bf16_bits(den == 0.0f ? 0.0f : x / den) |
-             ((uint32_t)float_to_bf16_bits(den == 0.0f ? 0.0f : y / den) << 16);
+    for (int k = 0; k < 8; ++k) x[k] = ored[0][r][d0 + k] + ored[1][r][d0 + k];
+    if (ks.pieces > 1) {
+      const int64_t piece = ((int64_t)(seq * p.kv.n_kv + j) * p.max_pieces + split) * p.max_rows + r;
+      float4* dst = reinterpret_cast<float4*>(p.part + piece * D + d0);
+      dst[0] = make_float4(x[0], x[1], x[2], x[3]);
+      dst[1] = make_float4(x[4], x[5], x[6], x[7]);
+      if (d0 == 0) p.part_ml[piece] = make_float2(mr, den);
+    } else {
+      uint32_t o[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        o[k] = (uint32_t)float_to_bf16_bits(den == 0.0f ? 0.0f : x[2 * k] / den) |
+               ((uint32_t)float_to_bf16_bits(den == 0.0f ? 0.0f : x[2 * k + 1] / den) << 16);
+      uint16_t* dst = p.out + (int64_t)(tl.q0 + r / p.group) * p.ldo + (int64_t)(j * p.group + r % p.group) * D + d0;
+      *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
     }
-    uint16_t* dst = p.out + (int64_t)(tl.q0 + r / p.group) * p.ldo + (int64_t)(j * p.group + r % p.group) * D + d0;
-    *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
   }
 }
 
-hipError_t launch_attn_paged(const PagedAttnParams& p, int head_dim, hipStream_t st) {
-  const dim3 g((unsigned)(p.rows * p.group / 16 + p.batch.n_seqs), (unsigned)p.kv.n_kv);
-  if (head_dim == 256)
-    p.kv.sk ? attn_paged_kernel<256, true><<<g, 256, 0, st>>>(p) : attn_paged_kernel<256, false><<<g, 256, 0, st>>>(p);
-  else
-    p.kv.sk ? attn_paged_kernel<128, true><<<g, 256, 0, st>>>(p) : attn_paged_kernel<128, false><<<g, 256, 0, st>>>(p);
+// The pieces of a row: thread (d, i) adds dimension d of the pieces i, i + G, ...
+// (all loads of eight at once), then the groups' sums are added in order.
+template <int D>
+__global__ __launch_bounds__(1024) void attn_join_kernel(PagedAttnParams p) {
+  constexpr int G = 1024 / D;
+  __shared__ float red[G][D];
+  Seq tl;
+  const int seq = blockIdx.x, j = blockIdx.y, r = blockIdx.z;
+  if (!seq_of(p, seq, &tl)) return;  // whole workgroup
+  const int rows = tl.q_len * p.group;
+  if (rows > p.max_rows || r >= rows) return;
+  const int pieces = keys_of(p, tl, 0, rows - 1, p.piece).pieces;
+  if (pieces == 1) return;  // written already
+  const int64_t base = (int64_t)(seq * p.kv.n_kv + j) * p.max_pieces * p.max_rows + r;
+  const int d = threadIdx.x % D, g = threadIdx.x / D;
+  float m = -INFINITY;
+  for (int i = lane_id(); i < pieces; i += kWave) m = fmaxf(m, p.part_ml[base + (int64_t)i * p.max_rows].x);
+  m = wave_max(m);
+  const float ref = m == -INFINITY ? 0.0f : m;
+  float den = 0.0f;
+  for (int i = lane_id(); i < pieces; i += kWave) {
+    const float2 ml = p.part_ml[base + (int64_t)i * p.max_rows];
+    den += ml.y * __builtin_amdgcn_exp2f(ml.x - ref);
+  }
+  den = wave_sum(den);
+  float o = 0.0f;
+#pragma unroll 8
+  for (int i = g; i < pieces; i += G) {
+    const int64_t at = base + (int64_t)i * p.max_rows;
+    o += p.part[at * D + d] * __builtin_amdgcn_exp2f(p.part_ml[at].x - ref);
+  }
+  red[g][d] = o;
+  __syncthreads();
+  if (g == 0) {
+#pragma unroll
+    for (int i = 1; i < G; ++i) o += red[i][d];
+    p.out[(int64_t)(tl.q0 + r / p.group) * p.ldo + (int64_t)(j * p.group + r % p.group) * D + d] =
+        float_to_bf16_bits(den == 0.0f ? 0.0f : o / den);
+  }
+}
+
+// ------------------------------------------------------------------ more than 16 rows
+
+constexpr int kTile = 128;     // rows of a workgroup
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+
+__device__ v4i kZeros = {0, 0, 0, 0};  // what stands for a row that is not read
+typedef const __attribute__((address_space(1))) v4i* GlobalVec;
+
+// A tile of a sequence of more than 16 rows.  Sequence s has the slots floor(q_start[s] *
+// group / kTile) + s and up, one for each of its tiles at least: a workgroup finds
+// its sequence without a prefix sum, and the slots left between are empty.
+__device__ __forceinline__ bool tile_of(const PagedAttnParams& p, int64_t slot, Seq* t, int* seq, int* row0) {
+  int count = 0;
+  for (int base = 0; base < p.batch.n_seqs; base += kWave) {
+    const int s = base + lane_id();
+    const uint64_t m = __ballot(s < p.batch.n_seqs && (int64_t)p.batch.q_start[min(s, p.batch.n_seqs)] * p.group / kTile + s <= slot);
+    count += __popcll(m);
+    if (m != ~0ull) break;
+  }
+  if (count == 0) return false;
+  *seq = count - 1;
+  if (!seq_of(p, count - 1, t)) return false;
+  const int64_t r = (slot - (int64_t)t->q0 * p.group / kTile - (count - 1)) * kTile, rows = (int64_t)t->q_len * p.group;
+  *row0 = (int)r;
+  return r >= 0 && r < rows && rows > kRows;
+}
+
+__device__ __forceinline__ v16f mma32_bf16(v4i a, v4i b, v16f c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+}
+// v of this lane and of the one 32 away
+__device__ __forceinline__ float max32(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum32(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  return (uint32_t)float_to_bf16_bits(lo) | ((uint32_t)float_to_bf16_bits(hi) << 16);
+}
+
+// 128 rows of a sequence.  Eight waves, four row groups of 32 rows times two key
+// groups: key group k takes the 32-key tiles k, k + 2, ... of the piece, from its
+// own half of LDS, where the tile after the present one is being put meanwhile.
+// With 32 x 32 products a wave's scores (keys x rows) leave each lane 16 keys of one
+// row; as bf16 they are the second operand of the value product (dimensions x
+// keys) times (keys x rows), whose first operand the transposing LDS read takes
+// from value rows as they lie.  Rows of a tile are D bf16 values, their 16-byte chunks
+// at index ^ (row % 8): both reads go evenly over the banks.  INT8 codes become
+// bf16 (exactly) on the way into LDS, once for the four row groups; a key's scale
+// multiplies its scores, a value's its weight.  The weights are rounded to bf16: 2^-9
+// on average of each, independent of each other, below the result's own rounding.
+// The reference of the exponentials follows the running maximum only when that
+// has grown by 2^8, so that the outputs are seldom rescaled (binary32 sums have the
+// room, and the rounding of the weights is relative).
+template <int D, bool I8>
+__global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
+  constexpr int NC = D / 16, NB = D / 32;  // 16-dimension steps of a score, 32-dimension blocks of a result
+  constexpr int ROWL = 2 * D, TILEB = kStep * ROWL;          // bytes of a row and of a tile in LDS
+  constexpr int ROWG = I8 ? D : 2 * D;                       // ... of a cached row
+  constexpr int LOADS = 8 * ROWG / 1024;                     // 16-byte loads of a lane for its wave's 8 rows
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  // [key group][buffer][key | value] tiles, then [key group][buffer][64] scales
+  float* scales = reinterpret_cast<float*>(smem + 8 * TILEB);
+
+  Seq tl;
+  int seq, row0;
+  const int64_t slot = (int64_t)gridDim.x - 1 - blockIdx.x;  // the longest ranges of keys first
+  const int j = blockIdx.y, split = blockIdx.z;
+  if (!tile_of(p, slot, &tl, &seq, &row0)) return;  // whole workgroup
+  const int rows = tl.q_len * p.group;
+  const Keys ks = keys_of(p, tl, row0, min(row0 + kTile, rows) - 1, p.tile_piece);
+  if (split >= ks.pieces) return;
+  const int begin = ks.begin + split * p.tile_piece, lo = ks.lo, hi = min(ks.hi, begin + p.tile_piece);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane_id(), n = l & 31, g = l >> 5;
+  const int rg = w & 3, kg = w >> 2;
+  const int wrow = row0 + 32 * rg, row = wrow + n;       // the wave's first row, the lane's row
+  const int pos = row < rows ? tl.first + row / p.group : -1;
+  const int from = pos < 0 ? 0 : max(0, pos + 1 - p.window);
+  const bool any = wrow < rows;                           // wave-uniform, as the next two
+  const int pos0 = tl.first + wrow / p.group, pos1 = tl.first + min(wrow + 31, rows - 1) / p.group;
+  const int32_t* table = p.batch.table + (int64_t)seq * p.batch.max_pages;
+  const int page_mask = (1 << p.kv.page_log2) - 1;
+
+  v4i q[NC];
+  {
+    const int r = min(row, rows - 1);
+    const uint16_t* src = p.q + (int64_t)(tl.q0 + r / p.group) * p.ldq + (int64_t)(j * p.group + r % p.group) * D + 8 * g;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) q[c] = *reinterpret_cast<const v4i*>(src + 16 * c);
+  }
+
+  char* const mine = smem + kg * 4 * TILEB;
+  v4i raw[I8 ? 2 * LOADS : 1];  // INT8: the next tile's codes
+  float raw_s = 0.0f;
+  bool held0 = false, held1 = false;  // of the tile last staged, by 16 keys
+  // The wave's 8 rows of the tile at k0 (they lie in one page) on their way to buffer b.
+  auto stage = [&](int k0, int b) {
+    const int id0 = k0 < hi ? table[k0 >> p.kv.page_log2] : -1, id1 = k0 + 16 < hi ? table[(k0 + 16) >> p.kv.page_log2] : -1;
+    held0 = id0 >= 0 && id0 < p.kv.n_pages;
+    held1 = id1 >= 0 && id1 < p.kv.n_pages;
+    const int id = rg >= 2 ? id1 : id0;
+    const bool held = rg >= 2 ? held1 : held0;
+    const int64_t at = held ? (((int64_t)id * p.kv.n_kv + j) << p.kv.page_log2) + ((k0 + 8 * rg) & page_mask) : 0;
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      const char* base = reinterpret_cast<const char*>(v ? p.kv.v : p.kv.k) + at * ROWG;
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int idx = 64 * i + l, r = idx / (ROWG / 16), c = idx % (ROWG / 16), key = k0 + 8 * rg + r;
+        const bool live = held && key >= lo && key < hi;
+        if constexpr (I8) {
+          const GlobalVec src = live ? (GlobalVec)(base + r * ROWG + 16 * c) : (GlobalVec)&kZeros;
+          raw[v * LOADS + i] = *src;
+        } else {
+          const GlobalVec src = live ? (GlobalVec)(base + r * ROWG + 16 * (c ^ r)) : (GlobalVec)&kZeros;
+          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                           (__attribute__((address_space(3))) void*)(mine + (2 * b + v) * TILEB + 8 * rg * ROWL + 1024 * i),
+                                           16, 0, 0);
+        }
+      }
+    }
+    if constexpr (I8) {
+      if (rg == 0) {  // scales: lane n of the keys, lane 32 + n of the values
+        const int key = k0 + n;
+        const bool live = (n < 16 ? held0 : held1) && key >= lo && key < hi;
+        const int64_t a = ((int64_t)((n < 16 ? id0 : id1)) * p.kv.n_kv + j) * (page_mask + 1) + (key & page_mask);
+        raw_s = live ? (g ? p.kv.sv : p.kv.sk)[a] : 0.0f;
+      }
+    }
+  };
+  // INT8: the staged codes into buffer b as bf16
+  auto put = [&](int b) {
+    if constexpr (I8) {
+#pragma unroll
+      for (int v = 0; v < 2; ++v)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          const int idx = 64 * i + l, r = idx / (ROWG / 16), c = idx % (ROWG / 16);
+          const v4i u = raw[v * LOADS + i];
+          const uint32_t x[4] = {(uint32_t)u.x, (uint32_t)u.y, (uint32_t)u.z, (uint32_t)u.w};
+          uint32_t o[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            o[2 * e] = (uint32_t)pair_hi(byte_f(x[e], 0), byte_f(x[e], 1));
+            o[2 * e + 1] = (uint32_t)pair_hi(byte_f(x[e], 2), byte_f(x[e], 3));
+          }
+          char* dst = mine + (2 * b + v) * TILEB + (8 * rg + r) * ROWL;
+          *reinterpret_cast<uint4*>(dst + 16 * ((2 * c) ^ r)) = make_uint4(o[0], o[1], o[2], o[3]);
+          *reinterpret_cast<uint4*>(dst + 16 * ((2 * c + 1) ^ r)) = make_uint4(o[4], o[5], o[6], o[7]);
+        }
+      if (rg == 0) scales[(kg * 2 + b) * 64 + l] = raw_s;
+    }
+  };
+
+  float ref = -INFINITY, sum = 0.0f;
+  v16f acc[NB];  // dimensions 32 b + 8 (r / 4) + 4 g + r % 4 of row n
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[b][r] = 0.0f;
+
+  // LDS addresses: chunk (2 c + g) ^ (n % 8) of key row n is 8 (c / 4) and one of four
+  // offsets; the value row's 8 (i / 2) and one of two
+  int koff[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) koff[c] = n * ROWL + 16 * ((2 * c + g) ^ (n & 7));
+  // value rows 16 h + 4 g + (l % 16) / 4 (and + 8), dimensions 32 i + 16 ((l / 16) % 2) + 4 (l % 4) .. + 3
+  const int vr = 4 * g + ((l >> 2) & 3), vchunk = 2 * ((l >> 4) & 1) + ((l >> 1) & 1);
+  const int voff[2] = {TILEB + vr * ROWL + 8 * (l & 1) + 16 * (vchunk ^ vr), TILEB + vr * ROWL + 8 * (l & 1) + 16 * ((4 + vchunk) ^ vr)};
+
+  // h0, h1: the two pages held; whole: every row attends every key
+  auto tile = [&](int k0, int b, bool h0, bool h1, bool whole) {
+    const char* buf = mine + 2 * b * TILEB;
+    v16f s;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      s = mma32_bf16(*reinterpret_cast<const v4i*>(buf + koff[c & 3] + 128 * (c >> 2)), q[c], s);
+    const float* sc = scales + (kg * 2 + b) * 64 + 4 * g;
+    float x[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = s[r] * p.scale_log2;
+    if constexpr (I8) {
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const float4 f = *reinterpret_cast<const float4*>(sc + 2 * r);
+        x[r] *= f.x; x[r + 1] *= f.y; x[r + 2] *= f.z; x[r + 3] *= f.w;
+      }
+    }
+    if (!whole) {  // keys from .. min(pos, hi - 1): one unsigned comparison each
+      const int span = min(pos, hi - 1) - from;
+      const uint32_t limit = (uint32_t)(span + 1), u = (uint32_t)(k0 + 4 * g - from);
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        x[r] = u + 8 * (r >> 2) + (r & 3) < (span >= 0 && (r < 8 ? h0 : h1) ? limit : 0u) ? x[r] : -INFINITY;
+    }
+    float mx = x[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
+    mx = max32(mx);
+    if (__any(mx > ref + 8.0f)) {
+      const float next = fmaxf(ref, mx), corr = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - next);
+      ref = next;
+      sum *= corr;
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][r] *= corr;
+    }
+    const float m = ref == -INFINITY ? 0.0f : ref;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      x[r] = __builtin_amdgcn_exp2f(x[r] - m);
+      sum += x[r];
+    }
+    if constexpr (I8) {
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const float4 f = *reinterpret_cast<const float4*>(sc + 32 + 2 * r);
+        x[r] *= f.x; x[r + 1] *= f.y; x[r + 2] *= f.z; x[r + 3] *= f.w;
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const v4i pw = {(int)pack2(x[8 * h], x[8 * h + 1]), (int)pack2(x[8 * h + 2], x[8 * h + 3]),
+                      (int)pack2(x[8 * h + 4], x[8 * h + 5]), (int)pack2(x[8 * h + 6], x[8 * h + 7])};
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const char* a = buf + voff[i & 1] + 16 * h * ROWL + 128 * (i >> 1);
+        typedef __attribute__((address_space(3))) v4s* lds4;
+        const v4s lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)a), hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(a + 8 * ROWL));
+        const int2 u = __builtin_bit_cast(int2, lo4), v = __builtin_bit_cast(int2, hi4);
+        acc[i] = mma32_bf16(v4i{u.x, u.y, v.x, v.y}, pw, acc[i]);
+      }
+    }
+  };
+
+  const int n_it = (hi - begin + 2 * kStep - 1) / (2 * kStep);
+  stage(begin + kStep * kg, 0);
+  put(0);
+  for (int it = 0; it < n_it; ++it) {
+    const int k0 = begin + kStep * (2 * it + kg), b = it & 1;
+    const bool here0 = held0, here1 = held1;
+    __builtin_amdgcn_s_waitcnt((15 << 8) | (7 << 4));  // this wave's loads into LDS
+    __syncthreads();
+    if (it + 1 < n_it) stage(k0 + 2 * kStep, b ^ 1);
+    if (any && k0 <= pos1 && k0 < hi && k0 + kStep > pos0 + 1 - p.window && (here0 || here1)) {
+      tile(k0, b, here0, here1, here0 && here1 && k0 + kStep - 1 <= pos0 && k0 > pos1 - p.window && k0 + kStep <= hi);
+    }
+    if (it + 1 < n_it) put(b ^ 1);
+  }
+
+  // ---- the two key groups
+  sum = sum32(sum);
+  __syncthreads();
+  float4* ex = reinterpret_cast<float4*>(smem) + rg * (64 * NB * 4);
+  float2* exm = reinterpret_cast<float2*>(smem + 8 * TILEB) ;  // where the scales were: 4 x 32 pairs
+  if (kg == 1) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        ex[(i * 4 + r / 4) * 64 + l] = make_float4(acc[i][r], acc[i][r + 1], acc[i][r + 2], acc[i][r + 3]);
+    if (g == 0) exm[32 * rg + n] = make_float2(ref, sum);
+  }
+  __syncthreads();
+  if (kg == 1 || !any) return;
+  const float2 o = exm[32 * rg + n];
+  const float top = fmaxf(ref, o.x), m = top == -INFINITY ? 0.0f : top;
+  const float f0 = __builtin_amdgcn_exp2f(ref - m), f1 = __builtin_amdgcn_exp2f(o.x - m);
+  sum = sum * f0 + o.y * f1;
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const int64_t part = (((int64_t)slot * p.kv.n_kv + j) * p.max_tile_pieces + split);
+  float4* dst = reinterpret_cast<float4*>(p.tile_part) + (part * 4 + rg) * (64 * NB * 4) + l;
+  uint16_t* out = p.out + (int64_t)(tl.q0 + row / p.group) * p.ldo + (int64_t)(j * p.group + row % p.group) * D + 4 * g;
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const float4 e = ex[(i * 4 + r / 4) * 64 + l];
+      const float4 x = make_float4(acc[i][r] * f0 + e.x * f1, acc[i][r + 1] * f0 + e.y * f1, acc[i][r + 2] * f0 + e.z * f1, acc[i][r + 3] * f0 + e.w * f1);
+      if (ks.pieces > 1)
+        dst[(i * 4 + r / 4) * 64] = x;
+      else if (row < rows)
+        *reinterpret_cast<uint2*>(out + 32 * i + 2 * r) = make_uint2(pack2(x.x * inv, x.y * inv), pack2(x.z * inv, x.w * inv));
+    }
+  if (ks.pieces > 1 && g == 0) p.tile_ml[part * kTile + 32 * rg + n] = make_float2(top, sum);
+}
+
+// The pieces of a tile: a workgroup joins 32 rows, each of its waves a quarter of
+// their dimensions, in the layout the pieces are in.
+template <int D>
+__global__ __launch_bounds__(256) void attn_tile_join_kernel(PagedAttnParams p) {
+  constexpr int NB = D / 32, Q = NB;  // float4 of a lane (NB * 4 / 4 waves)
+  Seq tl;
+  int seq, row0;
+  const int64_t slot = blockIdx.x;
+  const int j = blockIdx.y, rg = blockIdx.z, w = threadIdx.x >> 6, l = lane_id(), n = l & 31, g = l >> 5;
+  if (!tile_of(p, slot, &tl, &seq, &row0)) return;  // whole workgroup
+  const int rows = tl.q_len * p.group, row = row0 + 32 * rg + n;
+  if (row0 + 32 * rg >= rows) return;
+  const int pieces = keys_of(p, tl, row0, min(row0 + kTile, rows) - 1, p.tile_piece).pieces;
+  if (pieces == 1) return;  // written already
+  const int64_t part = ((int64_t)slot * p.kv.n_kv + j) * p.max_tile_pieces;
+  const float2* ml = p.tile_ml + part * kTile + 32 * rg + n;
+  const float4* src = reinterpret_cast<const float4*>(p.tile_part) + (part * 4 + rg) * (64 * NB * 4) + w * Q * 64 + l;
+  float top = -INFINITY, sum = 0.0f;
+  for (int i = 0; i < pieces; ++i) top = fmaxf(top, ml[(int64_t)i * kTile].x);
+  const float m = top == -INFINITY ? 0.0f : top;
+  float4 acc[Q];
+#pragma unroll
+  for (int k = 0; k < Q; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+  for (int i = 0; i < pieces; ++i) {
+    const float2 x = ml[(int64_t)i * kTile];
+    const float f = __builtin_amdgcn_exp2f(x.x - m);
+    sum += x.y * f;
+#pragma unroll
+    for (int k = 0; k < Q; ++k) {
+      const float4 v = src[(int64_t)i * 4 * (64 * NB * 4) + k * 64];
+      acc[k].x += v.x * f;
+      acc[k].y += v.y * f;
+      acc[k].z += v.z * f;
+      acc[k].w += v.w * f;
+    }
+  }
+  if (row >= rows) return;
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  uint16_t* out = p.out + (int64_t)(tl.q0 + row / p.group) * p.ldo + (int64_t)(j * p.group + row % p.group) * D + 4 * g;
+#pragma unroll
+  for (int k = 0; k < Q; ++k)  // float4 w * Q + k: dimensions 8 of it
+    *reinterpret_cast<uint2*>(out + 8 * (w * Q + k)) = make_uint2(pack2(acc[k].x * inv, acc[k].y * inv), pack2(acc[k].z * inv, acc[k].w * inv));
+}
+
+// ------------------------------------------------------------------ launches
+
+// Row kernel: as many pieces as give about four workgroups a CU if every context is
+// as long as it may be, of whole passes of the workgroup's waves (128 keys).
+static constexpr int kPieceTarget = 1024;
+// Tile kernel: pieces for one workgroup a CU at least, of 512 keys and more: a
+// piece writes its 128 rows in binary32 and they are read again to be joined.
+static constexpr int kTileTarget = 512, kTilePieceMin = 512;
+
+void attn_paged_plan(PagedAttnParams* p, int64_t max_q, int64_t ctx_max) {
+  const int64_t span = std::min<int64_t>(ctx_max, (int64_t)p->window + max_q) + kStep;  // keys of any row and its neighbours
+  p->max_q = (int)max_q;
+  p->max_rows = (int)std::min<int64_t>(max_q * p->group, kRows);
+  int64_t most = std::max<int64_t>(kPieceTarget / ((int64_t)p->batch.n_seqs * p->kv.n_kv), 1);
+  int64_t piece = (span + most - 1) / most;
+  piece = (piece + kPass - 1) / kPass * kPass;
+  p->piece = (int)piece;
+  p->max_pieces = (int)((span + piece - 1) / piece);
+  p->tile_slots = 0;
+  p->tile_piece = p->max_tile_pieces = 1;
+  if (max_q * p->group > kRows) {
+    p->tile_slots = (int)(p->rows * p->group / kTile + p->batch.n_seqs);
+    most = std::max<int64_t>(kTileTarget / ((p->rows * p->group / kTile + 1) * p->kv.n_kv), 1);
+    piece = std::max<int64_t>((span + most - 1) / most, kTilePieceMin);
+    piece = (piece + 2 * kStep - 1) / (2 * kStep) * (2 * kStep);
+    p->tile_piece = (int)piece;
+    p->max_tile_pieces = (int)((span + piece - 1) / piece);
+  }
+}
+
+// Workspace: outputs of the row kernel's pieces, of the tile kernel's, then their
+// maxima and sums.
+static size_t row_parts(const PagedAttnParams& p) {
+  return p.max_pieces == 1 ? 0 : (size_t)p.batch.n_seqs * p.kv.n_kv * p.max_pieces * p.max_rows;
+}
+static size_t tile_parts(const PagedAttnParams& p) {
+  return p.max_tile_pieces == 1 ? 0 : (size_t)p.tile_slots * p.kv.n_kv * p.max_tile_pieces * kTile;
+}
+size_t attn_paged_ws_bytes(const PagedAttnParams& p, int head_dim) {
+  return (row_parts(p) + tile_parts(p)) * (head_dim * sizeof(float) + sizeof(float2));
+}
+
+template <int D, bool I8>
+static hipError_t tile_launch(const PagedAttnParams& p, hipStream_t st) {
+  constexpr int kLds = 8 * kStep * 2 * D + 1024;
+  auto kern = attn_tile_kernel<D, I8>;
+  if constexpr (kLds > 64 * 1024) {
+    static bool attr_set[64] = {};  // by device; benign race: every caller sets the same value
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev >= 64 || !attr_set[dev]) {
+      e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+      if (e != hipSuccess) return e;
+      if (dev < 64) attr_set[dev] = true;
+    }
+  }
+  kern<<<dim3((unsigned)p.tile_slots, (unsigned)p.kv.n_kv, (unsigned)p.max_tile_pieces), 512, kLds, st>>>(p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.max_tile_pieces == 1) return e;
+  attn_tile_join_kernel<D><<<dim3((unsigned)p.tile_slots, (unsigned)p.kv.n_kv, 4), 256, 0, st>>>(p);
   return hipGetLastError();
+}
+
+template <int D, bool I8>
+static hipError_t paged_launch(PagedAttnParams p, void* ws, hipStream_t st) {
+  p.part = reinterpret_cast<float*>(ws);
+  p.tile_part = p.part + row_parts(p) * D;
+  p.part_ml = reinterpret_cast<float2*>(p.tile_part + tile_parts(p) * D);
+  p.tile_ml = p.part_ml + row_parts(p);
+  if (p.tile_slots) {
+    const hipError_t e = tile_launch<D, I8>(p, st);
+    if (e != hipSuccess) return e;
+  }
+  attn_rows_kernel<D, I8><<<dim3((unsigned)p.batch.n_seqs, (unsigned)p.kv.n_kv, (unsigned)p.max_pieces), 256, 0, st>>>(p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.max_pieces == 1) return e;
+  attn_join_kernel<D><<<dim3((unsigned)p.batch.n_seqs, (unsigned)p.kv.n_kv, (unsigned)p.max_rows), 1024, 0, st>>>(p);
+  return hipGetLastError();
+}
+
+hipError_t launch_attn_paged(const PagedAttnParams& p, int head_dim, void* ws, hipStream_t st) {
+  if (head_dim == 256) return p.kv.sk ? paged_launch<256, true>(p, ws, st) : paged_launch<256, false>(p, ws, st);
+  return p.kv.sk ? paged_launch<128, true>(p, ws, st) : paged_launch<128, false>(p, ws, st);
 }
 
 }  // namespace w8a8

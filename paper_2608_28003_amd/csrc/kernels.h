@@ -361,8 +361,20 @@ struct PagedAttnParams {
   float scale_log2 = 0.0f;        // score scale times log2(e)
   PagedKv kv;
   PagedBatch batch;
+  // set by attn_paged_plan: keys of a piece of the row kernel's work, most pieces
+  // and rows of a sequence; tiles of the tile kernel (0: not needed), the same of it
+  int max_q = 0, piece = 0, max_pieces = 0, max_rows = 0;
+  int tile_slots = 0, tile_piece = 0, max_tile_pieces = 0;
+  // set by the launcher: partial results
+  float* part = nullptr;
+  float* tile_part = nullptr;
+  float2* part_ml = nullptr;
+  float2* tile_ml = nullptr;
 };
-hipError_t launch_attn_paged(const PagedAttnParams& p, int head_dim, hipStream_t st);
+// the plan for sequences of at most max_q new tokens and ctx_max positions
+void attn_paged_plan(PagedAttnParams* p, int64_t max_q, int64_t ctx_max);
+size_t attn_paged_ws_bytes(const PagedAttnParams& p, int head_dim);  // of a planned call
+hipError_t launch_attn_paged(const PagedAttnParams& p, int head_dim, void* ws, hipStream_t st);
 
 // ------------------------------------------------------------------ sampling (sample.hip)
 

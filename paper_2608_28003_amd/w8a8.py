@@ -140,7 +140,7 @@ _SIGS = {
                              P]),
     "w8a8_kv_read": (INT, [ctypes.POINTER(PagedKvDesc), ctypes.POINTER(PagedBatchDesc), I64, P, P,
                            P]),
-    "w8a8_attn_paged_workspace_bytes": (SZ, [I64, I64, I64, I64, I64, I64, I64]),
+    "w8a8_attn_paged_workspace_bytes": (SZ, [I64, I64, I64, I64, I64, I64, I64, I64]),
     "w8a8_attn_paged": (INT, [P, I64, I64, I64, ctypes.POINTER(PagedKvDesc),
                               ctypes.POINTER(PagedBatchDesc), I64, ctypes.c_float, P, I64, P, SZ,
                               P]),
@@ -1011,8 +1011,10 @@ def kv_read(cache: PagedKV, batch: PagedBatch, rows, k=None, v=None, stream=None
     return k, v
 
 
-def attn_paged_workspace_bytes(rows, n_heads, n_kv, head_dim, n_seqs, max_q, ctx_max):
-    return lib().w8a8_attn_paged_workspace_bytes(rows, n_heads, n_kv, head_dim, n_seqs, max_q, ctx_max)
+def attn_paged_workspace_bytes(rows, n_heads, n_kv, head_dim, n_seqs, max_q, ctx_max, window=None):
+    """ctx_max: the positions that the tables can hold (max_pages * page)."""
+    return lib().w8a8_attn_paged_workspace_bytes(rows, n_heads, n_kv, head_dim, n_seqs, max_q,
+                                                 1 << 30 if window is None else window, ctx_max)
 
 
 def attn_paged(q, cache: PagedKV, batch: PagedBatch, window=None, scale=None, out=None, ws=None, stream=None):
@@ -1034,11 +1036,11 @@ def attn_paged(q, cache: PagedKV, batch: PagedBatch, window=None, scale=None, ou
         ldo = _row_stride(out, "out")
         if ws is None:
             ws = _empty(attn_paged_workspace_bytes(rows, heads, kv.n_kv, d, b.n_seqs, b.max_q,
-                                                   b.max_pages * kv.page), q.device)
+                                                   b.max_pages * kv.page, window), q.device)
         elif ws.device != q.device:
             raise ValueError("ws must be on q's device")
         _check(lib().w8a8_attn_paged(q.data_ptr(), rows, ldq, heads, ctypes.byref(kv), ctypes.byref(b),
-                                     2 ** 31 - 1 if window is None else window,
+                                     1 << 30 if window is None else window,
                                      d ** -0.5 if scale is None else scale, out.data_ptr(), ldo,
                                      ws.data_ptr(), ws.numel() * ws.element_size(), st))
     return out
