@@ -34,6 +34,10 @@ __device__ __forceinline__ int pair_hi(float lo, float hi) {
   return (int)__builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
 }
 
+// Arrays that no kernel writes, read through the scalar cache where the index is the
+// same for a wave.
+typedef const __attribute__((address_space(4))) int32_t* ConstInts;
+
 // The new tokens of sequence s, false where it has none (or its arrays are not
 // what they should be: rows outside the call, more tokens than the workspace is
 // for; those rows are not touched).
@@ -42,11 +46,12 @@ struct Seq {
   int first;  // position of the first new token
 };
 __device__ __forceinline__ bool seq_of(const PagedAttnParams& p, int s, Seq* t) {
-  const int q0 = p.batch.q_start[s], q1 = p.batch.q_start[s + 1];
+  const ConstInts start = (ConstInts)p.batch.q_start;
+  const int q0 = start[s], q1 = start[s + 1];
   if (q0 < 0 || q1 > p.rows || q1 <= q0 || q1 - q0 > p.max_q) return false;
   t->q0 = q0;
   t->q_len = q1 - q0;
-  t->first = max(p.batch.ctx_len[s], 0) - t->q_len;
+  t->first = max(((ConstInts)p.batch.ctx_len)[s], 0) - t->q_len;
   return true;
 }
 
@@ -97,7 +102,7 @@ __global__ __launch_bounds__(256, I8 ? 2 : 1) void attn_rows_kernel(PagedAttnPar
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = lane_id(), n = l & 15, g = l >> 4;
   const int pos = n < rows ? tl.first + n / p.group : -1;
   const int from = pos < 0 ? 0 : max(0, pos + 1 - p.window);
-  const int32_t* table = p.batch.table + (int64_t)seq * p.batch.max_pages;
+  const ConstInts table = (ConstInts)(p.batch.table + (int64_t)seq * p.batch.max_pages);
   const int page_mask = (1 << p.kv.page_log2) - 1;
 
   uint4 kc[2][KI];       // key row 16 t + n, bytes 64 i + 16 g .. + 15
@@ -371,6 +376,9 @@ __global__ __launch_bounds__(1024) void attn_join_kernel(PagedAttnParams p) {
 // ------------------------------------------------------------------ more than 16 rows
 
 constexpr int kTile = 128;     // rows of a workgroup
+// Products whose reads of LDS are on their way (left to itself the compiler, short of
+// registers, waits for every read).
+constexpr int kAhead = 3;
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 
@@ -389,6 +397,7 @@ __device__ __forceinline__ bool tile_of(const PagedAttnParams& p, int64_t slot, 
     if (m != ~0ull) break;
   }
   if (count == 0) return false;
+  count = __builtin_amdgcn_readfirstlane(count);
   *seq = count - 1;
   if (!seq_of(p, count - 1, t)) return false;
   const int64_t r = (slot - (int64_t)t->q0 * p.group / kTile - (count - 1)) * kTile, rows = (int64_t)t->q_len * p.group;
@@ -408,8 +417,28 @@ __device__ __forceinline__ float sum32(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  return (uint32_t)float_to_bf16_bits(lo) | ((uint32_t)float_to_bf16_bits(hi) << 16);
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {  // one v_cvt_pk_bf16_f32
+  return __builtin_bit_cast(uint32_t, v2bf{(__bf16)lo, (__bf16)hi});
+}
+// 16 bytes a lane from memory into LDS at `lds` (wave-uniform) + 16 * lane, without a
+// register.  In assembly because the compiler, which cannot tell the two buffers
+// apart, waits for the builtin's loads before the transposing reads of the present
+// tile; the wait is at the barrier that ends the buffer's filling.
+__device__ __forceinline__ void load_lds16(GlobalVec src, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(lds) : "memory");
+}
+// N such loads 1024 bytes apart, both in LDS and from `base` (wave-uniform); load i at
+// lane offset off ^ (step * i).
+template <int N>
+__device__ __forceinline__ void load_lds16_rows(const char* base, uint32_t off, uint32_t step, uint32_t lds) {
+  if constexpr (N == 4)
+    asm volatile("s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024\n\t"
+                 "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072"
+                 : : "v"(off), "v"(off ^ step), "v"(off ^ (2 * step)), "v"(off ^ (3 * step)), "s"(base), "s"(lds) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024"
+                 : : "v"(off), "v"(off ^ step), "s"(base), "s"(lds) : "memory");
 }
 
 // 128 rows of a sequence.  Eight waves, four row groups of 32 rows times two key
@@ -452,7 +481,7 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
   const int from = pos < 0 ? 0 : max(0, pos + 1 - p.window);
   const bool any = wrow < rows;                           // wave-uniform, as the next two
   const int pos0 = tl.first + wrow / p.group, pos1 = tl.first + min(wrow + 31, rows - 1) / p.group;
-  const int32_t* table = p.batch.table + (int64_t)seq * p.batch.max_pages;
+  const ConstInts table = (ConstInts)(p.batch.table + (int64_t)seq * p.batch.max_pages);
   const int page_mask = (1 << p.kv.page_log2) - 1;
 
   v4i q[NC];
@@ -464,37 +493,42 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
   }
 
   char* const mine = smem + kg * 4 * TILEB;
-  v4i raw[I8 ? 2 * LOADS : 1];  // INT8: the next tile's codes
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine + 8 * rg * ROWL;
+  // bf16: lane's offset into the wave's rows for load 0 (row l / chunks of a row, its
+  // chunk ^ row); load i is 1024 / ROWG rows on, which the rows' xor and 1024 bytes give
+  const uint32_t soff = (uint32_t)(l / (ROWG / 16) * ROWG + 16 * ((l % (ROWG / 16)) ^ (l / (ROWG / 16))));
+  v4i raw[I8 ? LOADS : 1];  // INT8: codes of the next tile's keys, then of its values
   float raw_s = 0.0f;
   bool held0 = false, held1 = false;  // of the tile last staged, by 16 keys
-  // The wave's 8 rows of the tile at k0 (they lie in one page) on their way to buffer b.
-  auto stage = [&](int k0, int b) {
-    const int id0 = k0 < hi ? table[k0 >> p.kv.page_log2] : -1, id1 = k0 + 16 < hi ? table[(k0 + 16) >> p.kv.page_log2] : -1;
+  int id0 = -1, id1 = -1;             // pages of the tile to be staged next
+  auto find = [&](int k0) {
+    id0 = k0 < hi ? table[k0 >> p.kv.page_log2] : -1;
+    id1 = k0 + 16 < hi ? table[(k0 + 16) >> p.kv.page_log2] : -1;
+  };
+  // The wave's 8 rows of the tile at k0 (they lie in one page) on their way to buffer
+  // b: keys (v = 0), values (v = 1).
+  auto stage = [&](int k0, int b, int v) {
     held0 = id0 >= 0 && id0 < p.kv.n_pages;
     held1 = id1 >= 0 && id1 < p.kv.n_pages;
     const int id = rg >= 2 ? id1 : id0;
     const bool held = rg >= 2 ? held1 : held0;
     const int64_t at = held ? (((int64_t)id * p.kv.n_kv + j) << p.kv.page_log2) + ((k0 + 8 * rg) & page_mask) : 0;
+    const char* base = reinterpret_cast<const char*>(v ? p.kv.v : p.kv.k) + at * ROWG;
+    if constexpr (I8) {  // whatever the rows hold: codes are finite, and what none attends has weight 0
 #pragma unroll
-    for (int v = 0; v < 2; ++v) {
-      const char* base = reinterpret_cast<const char*>(v ? p.kv.v : p.kv.k) + at * ROWG;
+      for (int i = 0; i < LOADS; ++i) raw[i] = *(GlobalVec)(base + (uint32_t)(16 * l) + 1024 * i);
+    } else if (held && k0 + 8 * rg >= lo && k0 + 8 * rg + 8 <= hi) {  // all of them; wave-uniform
+      load_lds16_rows<LOADS>(base, soff, 16 * (1024 / ROWG), lds0 + (2 * b + v) * TILEB);
+    } else {
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
         const int idx = 64 * i + l, r = idx / (ROWG / 16), c = idx % (ROWG / 16), key = k0 + 8 * rg + r;
-        const bool live = held && key >= lo && key < hi;
-        if constexpr (I8) {
-          const GlobalVec src = live ? (GlobalVec)(base + r * ROWG + 16 * c) : (GlobalVec)&kZeros;
-          raw[v * LOADS + i] = *src;
-        } else {
-          const GlobalVec src = live ? (GlobalVec)(base + r * ROWG + 16 * (c ^ r)) : (GlobalVec)&kZeros;
-          __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                           (__attribute__((address_space(3))) void*)(mine + (2 * b + v) * TILEB + 8 * rg * ROWL + 1024 * i),
-                                           16, 0, 0);
-        }
+        const GlobalVec src = held && key >= lo && key < hi ? (GlobalVec)(base + r * ROWG + 16 * (c ^ r)) : (GlobalVec)&kZeros;
+        load_lds16(src, lds0 + (2 * b + v) * TILEB + 1024 * i);
       }
     }
     if constexpr (I8) {
-      if (rg == 0) {  // scales: lane n of the keys, lane 32 + n of the values
+      if (rg == 0 && v == 0) {  // scales: lane n of the keys, lane 32 + n of the values
         const int key = k0 + n;
         const bool live = (n < 16 ? held0 : held1) && key >= lo && key < hi;
         const int64_t a = ((int64_t)((n < 16 ? id0 : id1)) * p.kv.n_kv + j) * (page_mask + 1) + (key & page_mask);
@@ -503,14 +537,12 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
     }
   };
   // INT8: the staged codes into buffer b as bf16
-  auto put = [&](int b) {
+  auto put = [&](int b, int v) {
     if constexpr (I8) {
-#pragma unroll
-      for (int v = 0; v < 2; ++v)
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
           const int idx = 64 * i + l, r = idx / (ROWG / 16), c = idx % (ROWG / 16);
-          const v4i u = raw[v * LOADS + i];
+          const v4i u = raw[i];
           const uint32_t x[4] = {(uint32_t)u.x, (uint32_t)u.y, (uint32_t)u.z, (uint32_t)u.w};
           uint32_t o[8];
 #pragma unroll
@@ -522,7 +554,7 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
           *reinterpret_cast<uint4*>(dst + 16 * ((2 * c) ^ r)) = make_uint4(o[0], o[1], o[2], o[3]);
           *reinterpret_cast<uint4*>(dst + 16 * ((2 * c + 1) ^ r)) = make_uint4(o[4], o[5], o[6], o[7]);
         }
-      if (rg == 0) scales[(kg * 2 + b) * 64 + l] = raw_s;
+      if (rg == 0 && v == 0) scales[(kg * 2 + b) * 64 + l] = raw_s;
     }
   };
 
@@ -533,24 +565,28 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[b][r] = 0.0f;
 
-  // LDS addresses: chunk (2 c + g) ^ (n % 8) of key row n is 8 (c / 4) and one of four
-  // offsets; the value row's 8 (i / 2) and one of two
-  int koff[4];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) koff[c] = n * ROWL + 16 * ((2 * c + g) ^ (n & 7));
-  // value rows 16 h + 4 g + (l % 16) / 4 (and + 8), dimensions 32 i + 16 ((l / 16) % 2) + 4 (l % 4) .. + 3
-  const int vr = 4 * g + ((l >> 2) & 3), vchunk = 2 * ((l >> 4) & 1) + ((l >> 1) & 1);
-  const int voff[2] = {TILEB + vr * ROWL + 8 * (l & 1) + 16 * (vchunk ^ vr), TILEB + vr * ROWL + 8 * (l & 1) + 16 * ((4 + vchunk) ^ vr)};
+  // LDS addresses: chunk (2 c + g) ^ (n % 8) of key row n is 8 (c / 4) + (g ^ (n % 8)) ^ (2 (c % 4));
+  // chunk (4 i + vchunk) ^ vr of a value row is 8 (i / 2) + (vchunk ^ vr) ^ (4 (i % 2)), for the
+  // rows 16 h + 4 g + (l % 16) / 4 (and + 8) and dimensions 32 i + 16 ((l / 16) % 2) + 4 (l % 4) .. + 3
+  const int vr = 4 * g + ((l >> 2) & 3);
+  const int koff = n * ROWL + 16 * (g ^ (n & 7));
+  const int voff = TILEB + vr * ROWL + 8 * (l & 1) + 16 * ((2 * ((l >> 4) & 1) + ((l >> 1) & 1)) ^ vr);
 
   // h0, h1: the two pages held; whole: every row attends every key
-  auto tile = [&](int k0, int b, bool h0, bool h1, bool whole) {
+  v4i pw[2];  // the weights of a tile
+  auto weights = [&](int k0, int b, bool h0, bool h1, bool whole) {
     const char* buf = mine + 2 * b * TILEB;
     v16f s;
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+    __builtin_amdgcn_sched_barrier(0);
+    v4i kf[kAhead];
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-      s = mma32_bf16(*reinterpret_cast<const v4i*>(buf + koff[c & 3] + 128 * (c >> 2)), q[c], s);
+    for (int c = 0; c < NC + kAhead; ++c) {  // the reads of kAhead products ahead
+      if (c >= kAhead) s = mma32_bf16(kf[c % kAhead], q[c - kAhead], s);
+      if (c < NC) kf[c % kAhead] = *reinterpret_cast<const v4i*>(buf + (koff ^ (32 * (c & 3))) + 128 * (c >> 2));
+      __builtin_amdgcn_sched_barrier(0);
+    }
     const float* sc = scales + (kg * 2 + b) * 64 + 4 * g;
     float x[16];
 #pragma unroll
@@ -596,38 +632,68 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
       }
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const v4i pw = {(int)pack2(x[8 * h], x[8 * h + 1]), (int)pack2(x[8 * h + 2], x[8 * h + 3]),
-                      (int)pack2(x[8 * h + 4], x[8 * h + 5]), (int)pack2(x[8 * h + 6], x[8 * h + 7])};
+    for (int h = 0; h < 2; ++h)
+      pw[h] = v4i{(int)pack2(x[8 * h], x[8 * h + 1]), (int)pack2(x[8 * h + 2], x[8 * h + 3]),
+                  (int)pack2(x[8 * h + 4], x[8 * h + 5]), (int)pack2(x[8 * h + 6], x[8 * h + 7])};
+  };
+  auto values = [&](int b) {
+    const char* buf = mine + 2 * b * TILEB;
+    __builtin_amdgcn_sched_barrier(0);
+    v4i vf[kAhead];
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const char* a = buf + voff[i & 1] + 16 * h * ROWL + 128 * (i >> 1);
+    for (int t = 0; t < 2 * NB + kAhead; ++t) {
+      const int u = t - kAhead;
+      if (u >= 0) acc[u % NB] = mma32_bf16(vf[u % kAhead], pw[u / NB], acc[u % NB]);
+      if (t < 2 * NB) {
+        const int h = t / NB, i = t % NB;
+        const char* a = buf + (voff ^ (64 * (i & 1))) + 16 * h * ROWL + 128 * (i >> 1);
         typedef __attribute__((address_space(3))) v4s* lds4;
         const v4s lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)a), hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(a + 8 * ROWL));
-        const int2 u = __builtin_bit_cast(int2, lo4), v = __builtin_bit_cast(int2, hi4);
-        acc[i] = mma32_bf16(v4i{u.x, u.y, v.x, v.y}, pw, acc[i]);
+        const int2 x = __builtin_bit_cast(int2, lo4), y = __builtin_bit_cast(int2, hi4);
+        vf[t % kAhead] = v4i{x.x, x.y, y.x, y.y};
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
 
   const int n_it = (hi - begin + 2 * kStep - 1) / (2 * kStep);
-  stage(begin + kStep * kg, 0);
-  put(0);
+  find(begin + kStep * kg);
+  stage(begin + kStep * kg, 0, 0);
+  put(0, 0);
+  stage(begin + kStep * kg, 0, 1);
+  put(0, 1);
+  find(begin + kStep * (kg + 2));
   for (int it = 0; it < n_it; ++it) {
     const int k0 = begin + kStep * (2 * it + kg), b = it & 1;
     const bool here0 = held0, here1 = held1;
     __builtin_amdgcn_s_waitcnt((15 << 8) | (7 << 4));  // this wave's loads into LDS
     __syncthreads();
-    if (it + 1 < n_it) stage(k0 + 2 * kStep, b ^ 1);
-    if (any && k0 <= pos1 && k0 < hi && k0 + kStep > pos0 + 1 - p.window && (here0 || here1)) {
-      tile(k0, b, here0, here1, here0 && here1 && k0 + kStep - 1 <= pos0 && k0 > pos1 - p.window && k0 + kStep <= hi);
+    // the next tile: bf16 straight into LDS; INT8 through the same registers, the
+    // keys while the scores are formed, the values during the value product
+    if constexpr (I8) {
+      stage(k0 + 2 * kStep, b ^ 1, 0);  // past the end: page 0, for nothing
+    } else if (it + 1 < n_it) {
+      stage(k0 + 2 * kStep, b ^ 1, 0);
+      stage(k0 + 2 * kStep, b ^ 1, 1);
     }
-    if (it + 1 < n_it) put(b ^ 1);
+    const bool seen = any && k0 <= pos1 && k0 < hi && k0 + kStep > pos0 + 1 - p.window && (here0 || here1);
+    if (seen) weights(k0, b, here0, here1, here0 && here1 && k0 + kStep - 1 <= pos0 && k0 > pos1 - p.window && k0 + kStep <= hi);
+    if constexpr (I8) {
+      put(b ^ 1, 0);
+      stage(k0 + 2 * kStep, b ^ 1, 1);
+    }
+    if (seen) values(b);
+    find(k0 + 4 * kStep);
+    put(b ^ 1, 1);
   }
 
   // ---- the two key groups
   sum = sum32(sum);
   __syncthreads();
+  int lane = threadIdx.x;  // from here on: what the loop need not hold registers for
+  asm volatile("" : "+v"(lane));
+  lane &= 63;
+  const int ln = lane & 31, lg = lane >> 5, lrow = wrow + ln;
   float4* ex = reinterpret_cast<float4*>(smem) + rg * (64 * NB * 4);
   float2* exm = reinterpret_cast<float2*>(smem + 8 * TILEB) ;  // where the scales were: 4 x 32 pairs
   if (kg == 1) {
@@ -635,31 +701,31 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
     for (int i = 0; i < NB; ++i)
 #pragma unroll
       for (int r = 0; r < 16; r += 4)
-        ex[(i * 4 + r / 4) * 64 + l] = make_float4(acc[i][r], acc[i][r + 1], acc[i][r + 2], acc[i][r + 3]);
-    if (g == 0) exm[32 * rg + n] = make_float2(ref, sum);
+        ex[(i * 4 + r / 4) * 64 + lane] = make_float4(acc[i][r], acc[i][r + 1], acc[i][r + 2], acc[i][r + 3]);
+    if (lg == 0) exm[32 * rg + ln] = make_float2(ref, sum);
   }
   __syncthreads();
   if (kg == 1 || !any) return;
-  const float2 o = exm[32 * rg + n];
+  const float2 o = exm[32 * rg + ln];
   const float top = fmaxf(ref, o.x), m = top == -INFINITY ? 0.0f : top;
   const float f0 = __builtin_amdgcn_exp2f(ref - m), f1 = __builtin_amdgcn_exp2f(o.x - m);
   sum = sum * f0 + o.y * f1;
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   const int64_t part = (((int64_t)slot * p.kv.n_kv + j) * p.max_tile_pieces + split);
-  float4* dst = reinterpret_cast<float4*>(p.tile_part) + (part * 4 + rg) * (64 * NB * 4) + l;
-  uint16_t* out = p.out + (int64_t)(tl.q0 + row / p.group) * p.ldo + (int64_t)(j * p.group + row % p.group) * D + 4 * g;
+  float4* dst = reinterpret_cast<float4*>(p.tile_part) + (part * 4 + rg) * (64 * NB * 4) + lane;
+  uint16_t* out = p.out + (int64_t)(tl.q0 + lrow / p.group) * p.ldo + (int64_t)(j * p.group + lrow % p.group) * D + 4 * lg;
 #pragma unroll
   for (int i = 0; i < NB; ++i)
 #pragma unroll
     for (int r = 0; r < 16; r += 4) {
-      const float4 e = ex[(i * 4 + r / 4) * 64 + l];
+      const float4 e = ex[(i * 4 + r / 4) * 64 + lane];
       const float4 x = make_float4(acc[i][r] * f0 + e.x * f1, acc[i][r + 1] * f0 + e.y * f1, acc[i][r + 2] * f0 + e.z * f1, acc[i][r + 3] * f0 + e.w * f1);
       if (ks.pieces > 1)
         dst[(i * 4 + r / 4) * 64] = x;
-      else if (row < rows)
+      else if (lrow < rows)
         *reinterpret_cast<uint2*>(out + 32 * i + 2 * r) = make_uint2(pack2(x.x * inv, x.y * inv), pack2(x.z * inv, x.w * inv));
     }
-  if (ks.pieces > 1 && g == 0) p.tile_ml[part * kTile + 32 * rg + n] = make_float2(top, sum);
+  if (ks.pieces > 1 && lg == 0) p.tile_ml[part * kTile + 32 * rg + ln] = make_float2(top, sum);
 }
 
 // The pieces of a tile: a workgroup joins 32 rows, each of its waves a quarter of
@@ -729,7 +795,8 @@ void attn_paged_plan(PagedAttnParams* p, int64_t max_q, int64_t ctx_max) {
   p->tile_piece = p->max_tile_pieces = 1;
   if (max_q * p->group > kRows) {
     p->tile_slots = (int)(p->rows * p->group / kTile + p->batch.n_seqs);
-    most = std::max<int64_t>(kTileTarget / ((p->rows * p->group / kTile + 1) * p->kv.n_kv), 1);
+    const int64_t tiles = (p->rows * p->group / kTile + 1) * p->kv.n_kv;
+    most = (kTileTarget + tiles - 1) / tiles;
     piece = std::max<int64_t>((span + most - 1) / most, kTilePieceMin);
     piece = (piece + 2 * kStep - 1) / (2 * kStep) * (2 * kStep);
     p->tile_piece = (int)piece;
