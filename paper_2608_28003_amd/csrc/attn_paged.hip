@@ -417,6 +417,12 @@ __device__ __forceinline__ float sum32(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+// v, as something that the compiler cannot form ahead of the loop: what a single
+// instruction makes of it would be held in a register each.
+__device__ __forceinline__ int here(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {  // one v_cvt_pk_bf16_f32
   return __builtin_bit_cast(uint32_t, v2bf{(__bf16)lo, (__bf16)hi});
@@ -429,26 +435,27 @@ __device__ __forceinline__ void load_lds16(GlobalVec src, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(lds) : "memory");
 }
 // N such loads 1024 bytes apart, both in LDS and from `base` (wave-uniform); load i at
-// lane offset off ^ (step * i).
+// lane offset off ^ (s1 if i is odd) ^ (s2 if i >= 2).
 template <int N>
-__device__ __forceinline__ void load_lds16_rows(const char* base, uint32_t off, uint32_t step, uint32_t lds) {
+__device__ __forceinline__ void load_lds16_rows(const char* base, uint32_t off, uint32_t s1, uint32_t s2, uint32_t lds) {
   if constexpr (N == 4)
     asm volatile("s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024\n\t"
                  "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072"
-                 : : "v"(off), "v"(off ^ step), "v"(off ^ (2 * step)), "v"(off ^ (3 * step)), "s"(base), "s"(lds) : "memory");
+                 : : "v"(off), "v"(off ^ s1), "v"(off ^ s2), "v"(off ^ s1 ^ s2), "s"(base), "s"(lds) : "memory");
   else
     asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024"
-                 : : "v"(off), "v"(off ^ step), "s"(base), "s"(lds) : "memory");
+                 : : "v"(off), "v"(off ^ s1), "s"(base), "s"(lds) : "memory");
 }
-
 // 128 rows of a sequence.  Eight waves, four row groups of 32 rows times two key
 // groups: key group k takes the 32-key tiles k, k + 2, ... of the piece, from its
 // own half of LDS, where the tile after the present one is being put meanwhile.
 // With 32 x 32 products a wave's scores (keys x rows) leave each lane 16 keys of one
 // row; as bf16 they are the second operand of the value product (dimensions x
 // keys) times (keys x rows), whose first operand the transposing LDS read takes
-// from value rows as they lie.  Rows of a tile are D bf16 values, their 16-byte chunks
-// at index ^ (row % 8): both reads go evenly over the banks.  INT8 codes become
+// from value rows as they lie.  Rows of a tile are D bf16 values, the 16-byte chunks of
+// a key row at index ^ (row % 16), of a value row at index ^ (4 (row % 4)), so that
+// what is read in one cycle (the same chunk of 16 key rows; 64 bytes of four value
+// rows) covers the 64 banks once.  INT8 codes become
 // bf16 (exactly) on the way into LDS, once for the four row groups; a key's scale
 // multiplies its scores, a value's its weight.  The weights are rounded to bf16: 2^-9
 // on average of each, independent of each other, below the result's own rounding.
@@ -494,9 +501,9 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
 
   char* const mine = smem + kg * 4 * TILEB;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mine + 8 * rg * ROWL;
-  // bf16: lane's offset into the wave's rows for load 0 (row l / chunks of a row, its
-  // chunk ^ row); load i is 1024 / ROWG rows on, which the rows' xor and 1024 bytes give
-  const uint32_t soff = (uint32_t)(l / (ROWG / 16) * ROWG + 16 * ((l % (ROWG / 16)) ^ (l / (ROWG / 16))));
+  // where chunk 0 of row r of a tile lies in it: v = 0 keys, 1 values (the rest by xor)
+  auto swizzle = [](int r, int v) { return v ? 4 * (r & 3) : r & 15; };
+  constexpr int kChunks = ROWL / 16, kRowsLoad = 64 / kChunks;  // bf16: rows of a load
   v4i raw[I8 ? LOADS : 1];  // INT8: codes of the next tile's keys, then of its values
   float raw_s = 0.0f;
   bool held0 = false, held1 = false;  // of the tile last staged, by 16 keys
@@ -518,12 +525,14 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) raw[i] = *(GlobalVec)(base + (uint32_t)(16 * l) + 1024 * i);
     } else if (held && k0 + 8 * rg >= lo && k0 + 8 * rg + 8 <= hi) {  // all of them; wave-uniform
-      load_lds16_rows<LOADS>(base, soff, 16 * (1024 / ROWG), lds0 + (2 * b + v) * TILEB);
+      const int ln = here(l), r = ln / kChunks;
+      load_lds16_rows<LOADS>(base, r * ROWG + 16 * ((ln % kChunks) ^ swizzle(8 * rg + r, v)), 16 * swizzle(kRowsLoad, v),
+                             16 * swizzle(2 * kRowsLoad, v), lds0 + (2 * b + v) * TILEB);
     } else {
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
-        const int idx = 64 * i + l, r = idx / (ROWG / 16), c = idx % (ROWG / 16), key = k0 + 8 * rg + r;
-        const GlobalVec src = held && key >= lo && key < hi ? (GlobalVec)(base + r * ROWG + 16 * (c ^ r)) : (GlobalVec)&kZeros;
+        const int idx = 64 * i + here(l), r = idx / kChunks, c = idx % kChunks, key = k0 + 8 * rg + r;
+        const GlobalVec src = held && key >= lo && key < hi ? (GlobalVec)(base + r * ROWG + 16 * (c ^ swizzle(8 * rg + r, v))) : (GlobalVec)&kZeros;
         load_lds16(src, lds0 + (2 * b + v) * TILEB + 1024 * i);
       }
     }
@@ -541,7 +550,7 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
     if constexpr (I8) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-          const int idx = 64 * i + l, r = idx / (ROWG / 16), c = idx % (ROWG / 16);
+          const int idx = 64 * i + here(l), r = idx / (ROWG / 16), c = idx % (ROWG / 16);
           const v4i u = raw[i];
           const uint32_t x[4] = {(uint32_t)u.x, (uint32_t)u.y, (uint32_t)u.z, (uint32_t)u.w};
           uint32_t o[8];
@@ -551,8 +560,9 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
             o[2 * e + 1] = (uint32_t)pair_hi(byte_f(x[e], 2), byte_f(x[e], 3));
           }
           char* dst = mine + (2 * b + v) * TILEB + (8 * rg + r) * ROWL;
-          *reinterpret_cast<uint4*>(dst + 16 * ((2 * c) ^ r)) = make_uint4(o[0], o[1], o[2], o[3]);
-          *reinterpret_cast<uint4*>(dst + 16 * ((2 * c + 1) ^ r)) = make_uint4(o[4], o[5], o[6], o[7]);
+          const int z = swizzle(8 * rg + r, v);
+          *reinterpret_cast<uint4*>(dst + 16 * ((2 * c) ^ z)) = make_uint4(o[0], o[1], o[2], o[3]);
+          *reinterpret_cast<uint4*>(dst + 16 * ((2 * c + 1) ^ z)) = make_uint4(o[4], o[5], o[6], o[7]);
         }
       if (rg == 0 && v == 0) scales[(kg * 2 + b) * 64 + l] = raw_s;
     }
@@ -565,12 +575,12 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[b][r] = 0.0f;
 
-  // LDS addresses: chunk (2 c + g) ^ (n % 8) of key row n is 8 (c / 4) + (g ^ (n % 8)) ^ (2 (c % 4));
-  // chunk (4 i + vchunk) ^ vr of a value row is 8 (i / 2) + (vchunk ^ vr) ^ (4 (i % 2)), for the
-  // rows 16 h + 4 g + (l % 16) / 4 (and + 8) and dimensions 32 i + 16 ((l / 16) % 2) + 4 (l % 4) .. + 3
+  // LDS addresses: chunk 2 c + g of key row n, at (2 c + g) ^ (n % 16); chunk 4 i + low of
+  // the value rows vr = 4 g + (l % 16) / 4 (+ 8, + 16 h), at (4 i + low) ^ (4 (vr % 4)), whose
+  // four dimensions are 32 i + 16 ((l / 16) % 2) + 4 (l % 4) and up
   const int vr = 4 * g + ((l >> 2) & 3);
-  const int koff = n * ROWL + 16 * (g ^ (n & 7));
-  const int voff = TILEB + vr * ROWL + 8 * (l & 1) + 16 * ((2 * ((l >> 4) & 1) + ((l >> 1) & 1)) ^ vr);
+  const int koff = n * ROWL + 16 * (g ^ (n & 15));
+  const int voff = TILEB + vr * ROWL + 8 * (l & 1) + 16 * (2 * ((l >> 4) & 1) + ((l >> 1) & 1)) + 64 * (vr & 3);
 
   // h0, h1: the two pages held; whole: every row attends every key
   v4i pw[2];  // the weights of a tile
@@ -581,10 +591,11 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
     for (int r = 0; r < 16; ++r) s[r] = 0.0f;
     __builtin_amdgcn_sched_barrier(0);
     v4i kf[kAhead];
+    const int ko = here(koff);
 #pragma unroll
     for (int c = 0; c < NC + kAhead; ++c) {  // the reads of kAhead products ahead
       if (c >= kAhead) s = mma32_bf16(kf[c % kAhead], q[c - kAhead], s);
-      if (c < NC) kf[c % kAhead] = *reinterpret_cast<const v4i*>(buf + (koff ^ (32 * (c & 3))) + 128 * (c >> 2));
+      if (c < NC) kf[c % kAhead] = *reinterpret_cast<const v4i*>(buf + (ko ^ (32 * (c & 7))) + 256 * (c >> 3));
       __builtin_amdgcn_sched_barrier(0);
     }
     const float* sc = scales + (kg * 2 + b) * 64 + 4 * g;
@@ -640,13 +651,14 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
     const char* buf = mine + 2 * b * TILEB;
     __builtin_amdgcn_sched_barrier(0);
     v4i vf[kAhead];
+    const int vo = here(voff);
 #pragma unroll
     for (int t = 0; t < 2 * NB + kAhead; ++t) {
       const int u = t - kAhead;
       if (u >= 0) acc[u % NB] = mma32_bf16(vf[u % kAhead], pw[u / NB], acc[u % NB]);
       if (t < 2 * NB) {
         const int h = t / NB, i = t % NB;
-        const char* a = buf + (voff ^ (64 * (i & 1))) + 16 * h * ROWL + 128 * (i >> 1);
+        const char* a = buf + (vo ^ (64 * (i & 3))) + 16 * h * ROWL + 256 * (i >> 2);
         typedef __attribute__((address_space(3))) v4s* lds4;
         const v4s lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)a), hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(a + 8 * ROWL));
         const int2 x = __builtin_bit_cast(int2, lo4), y = __builtin_bit_cast(int2, hi4);
@@ -665,7 +677,7 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
   find(begin + kStep * (kg + 2));
   for (int it = 0; it < n_it; ++it) {
     const int k0 = begin + kStep * (2 * it + kg), b = it & 1;
-    const bool here0 = held0, here1 = held1;
+    const bool now0 = held0, now1 = held1;
     __builtin_amdgcn_s_waitcnt((15 << 8) | (7 << 4));  // this wave's loads into LDS
     __syncthreads();
     // the next tile: bf16 straight into LDS; INT8 through the same registers, the
@@ -676,8 +688,8 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
       stage(k0 + 2 * kStep, b ^ 1, 0);
       stage(k0 + 2 * kStep, b ^ 1, 1);
     }
-    const bool seen = any && k0 <= pos1 && k0 < hi && k0 + kStep > pos0 + 1 - p.window && (here0 || here1);
-    if (seen) weights(k0, b, here0, here1, here0 && here1 && k0 + kStep - 1 <= pos0 && k0 > pos1 - p.window && k0 + kStep <= hi);
+    const bool seen = any && k0 <= pos1 && k0 < hi && k0 + kStep > pos0 + 1 - p.window && (now0 || now1);
+    if (seen) weights(k0, b, now0, now1, now0 && now1 && k0 + kStep - 1 <= pos0 && k0 > pos1 - p.window && k0 + kStep <= hi);
     if constexpr (I8) {
       put(b ^ 1, 0);
       stage(k0 + 2 * kStep, b ^ 1, 1);
