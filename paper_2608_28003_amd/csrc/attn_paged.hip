@@ -13,6 +13,7 @@
 // second operand of the transposed value product, values x weights, as they
 // stand.  Maximum, sum and outputs run in binary32 along the keys.
 #include <algorithm>
+#include <type_traits>
 
 #include "device.h"
 #include "kernels.h"
@@ -376,9 +377,6 @@ __global__ __launch_bounds__(1024) void attn_join_kernel(PagedAttnParams p) {
 // ------------------------------------------------------------------ more than 16 rows
 
 constexpr int kTile = 128;     // rows of a workgroup
-// Products whose reads of LDS are on their way (left to itself the compiler, short of
-// registers, waits for every read).
-constexpr int kAhead = 3;
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 
@@ -432,12 +430,17 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {  // one v_cvt_pk
 // apart, waits for the builtin's loads before the transposing reads of the present
 // tile; the wait is at the barrier that ends the buffer's filling.
 __device__ __forceinline__ void load_lds16(GlobalVec src, uint32_t lds) {
+  lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(lds) : "memory");
 }
-// N such loads 1024 bytes apart, both in LDS and from `base` (wave-uniform); load i at
+// N such loads 1024 bytes apart, both in LDS and from `from` (wave-uniform); load i at
 // lane offset off ^ (s1 if i is odd) ^ (s2 if i >= 2).
 template <int N>
-__device__ __forceinline__ void load_lds16_rows(const char* base, uint32_t off, uint32_t s1, uint32_t s2, uint32_t lds) {
+__device__ __forceinline__ void load_lds16_rows(const char* from, uint32_t off, uint32_t s1, uint32_t s2, uint32_t lds) {
+  const uint64_t f = (uint64_t)(uintptr_t)from;
+  const uint64_t base = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(f >> 32)) << 32) |
+                        (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)f);
+  lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
   if constexpr (N == 4)
     asm volatile("s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024\n\t"
                  "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072"
@@ -469,7 +472,7 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
   constexpr int ROWG = I8 ? D : 2 * D;                       // ... of a cached row
   constexpr int LOADS = 8 * ROWG / 1024;                     // 16-byte loads of a lane for its wave's 8 rows
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  // [key group][buffer][key | value] tiles, then [key group][buffer][64] scales
+  // [key group][buffer][key | value] tiles, then [key group][tile % 4][keys' 32 | values' 32] scales
   float* scales = reinterpret_cast<float*>(smem + 8 * TILEB);
 
   Seq tl;
@@ -491,12 +494,15 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
   const ConstInts table = (ConstInts)(p.batch.table + (int64_t)seq * p.batch.max_pages);
   const int page_mask = (1 << p.kv.page_log2) - 1;
 
+  // maxima are taken of unscaled scores: a negative scale's sign goes into the queries
+  const float scale = fabsf(p.scale_log2);
+  const int flip = p.scale_log2 < 0.0f ? (int)0x80008000u : 0;
   v4i q[NC];
   {
     const int r = min(row, rows - 1);
     const uint16_t* src = p.q + (int64_t)(tl.q0 + r / p.group) * p.ldq + (int64_t)(j * p.group + r % p.group) * D + 8 * g;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) q[c] = *reinterpret_cast<const v4i*>(src + 16 * c);
+    for (int c = 0; c < NC; ++c) q[c] = *reinterpret_cast<const v4i*>(src + 16 * c) ^ flip;
   }
 
   char* const mine = smem + kg * 4 * TILEB;
@@ -504,67 +510,75 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
   // where chunk 0 of row r of a tile lies in it: v = 0 keys, 1 values (the rest by xor)
   auto swizzle = [](int r, int v) { return v ? 4 * (r & 3) : r & 15; };
   constexpr int kChunks = ROWL / 16, kRowsLoad = 64 / kChunks;  // bf16: rows of a load
-  v4i raw[I8 ? LOADS : 1];  // INT8: codes of the next tile's keys, then of its values
-  float raw_s = 0.0f;
-  bool held0 = false, held1 = false;  // of the tile last staged, by 16 keys
-  int id0 = -1, id1 = -1;             // pages of the tile to be staged next
-  auto find = [&](int k0) {
-    id0 = k0 < hi ? table[k0 >> p.kv.page_log2] : -1;
-    id1 = k0 + 16 < hi ? table[(k0 + 16) >> p.kv.page_log2] : -1;
+  v4i raw[I8 ? 2 * LOADS : 1];  // INT8: codes on their way, keys then values
+  float raw_s = 0.0f;           // and scales: lane n of the keys, lane 32 + n of the values
+  // pages of the two halves of a tile; -1 past the end or not held
+  struct Pages {
+    int a, b;
   };
+  auto page_at = [&](int k0) {
+    const int id = k0 < hi ? table[k0 >> p.kv.page_log2] : -1;
+    return id < p.kv.n_pages ? max(id, -1) : -1;
+  };
+  auto pages = [&](int k0) { return Pages{page_at(k0), page_at(k0 + 16)}; };
   // The wave's 8 rows of the tile at k0 (they lie in one page) on their way to buffer
   // b: keys (v = 0), values (v = 1).
-  auto stage = [&](int k0, int b, int v) {
-    held0 = id0 >= 0 && id0 < p.kv.n_pages;
-    held1 = id1 >= 0 && id1 < p.kv.n_pages;
-    const int id = rg >= 2 ? id1 : id0;
-    const bool held = rg >= 2 ? held1 : held0;
-    const int64_t at = held ? (((int64_t)id * p.kv.n_kv + j) << p.kv.page_log2) + ((k0 + 8 * rg) & page_mask) : 0;
+  auto stage = [&](int k0, Pages pg, int b, int v) {
+    const int id = rg >= 2 ? pg.b : pg.a, key = k0 + 8 * rg;
+    const int64_t at = (((int64_t)max(id, 0) * p.kv.n_kv + j) << p.kv.page_log2) + (key & page_mask);
     const char* base = reinterpret_cast<const char*>(v ? p.kv.v : p.kv.k) + at * ROWG;
     if constexpr (I8) {  // whatever the rows hold: codes are finite, and what none attends has weight 0
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) raw[i] = *(GlobalVec)(base + (uint32_t)(16 * l) + 1024 * i);
-    } else if (held && k0 + 8 * rg >= lo && k0 + 8 * rg + 8 <= hi) {  // all of them; wave-uniform
+      for (int i = 0; i < LOADS; ++i) raw[v * LOADS + i] = *(GlobalVec)(base + (uint32_t)(16 * l) + 1024 * i);
+    } else if (id >= 0 && key >= lo && key + 8 <= hi) {  // all of them; wave-uniform
       const int ln = here(l), r = ln / kChunks;
       load_lds16_rows<LOADS>(base, r * ROWG + 16 * ((ln % kChunks) ^ swizzle(8 * rg + r, v)), 16 * swizzle(kRowsLoad, v),
                              16 * swizzle(2 * kRowsLoad, v), lds0 + (2 * b + v) * TILEB);
     } else {
-#pragma unroll
+#pragma unroll 1
       for (int i = 0; i < LOADS; ++i) {
-        const int idx = 64 * i + here(l), r = idx / kChunks, c = idx % kChunks, key = k0 + 8 * rg + r;
-        const GlobalVec src = held && key >= lo && key < hi ? (GlobalVec)(base + r * ROWG + 16 * (c ^ swizzle(8 * rg + r, v))) : (GlobalVec)&kZeros;
+        const int idx = 64 * i + l, r = idx / kChunks, c = idx % kChunks;
+        const GlobalVec src = id >= 0 && key + r >= lo && key + r < hi ? (GlobalVec)(base + r * ROWG + 16 * (c ^ swizzle(8 * rg + r, v))) : (GlobalVec)&kZeros;
         load_lds16(src, lds0 + (2 * b + v) * TILEB + 1024 * i);
       }
     }
+  };
+  // INT8: scales of the keys at k0 and of the values at v0
+  auto stage_scales = [&](int k0, Pages pk, int v0, Pages pv) {
     if constexpr (I8) {
-      if (rg == 0 && v == 0) {  // scales: lane n of the keys, lane 32 + n of the values
-        const int key = k0 + n;
-        const bool live = (n < 16 ? held0 : held1) && key >= lo && key < hi;
-        const int64_t a = ((int64_t)((n < 16 ? id0 : id1)) * p.kv.n_kv + j) * (page_mask + 1) + (key & page_mask);
+      if (rg == 0) {
+        const int key = (g ? v0 : k0) + n, id = g ? (n < 16 ? pv.a : pv.b) : (n < 16 ? pk.a : pk.b);
+        const bool live = id >= 0 && key >= lo && key < hi;
+        const int64_t a = ((int64_t)id * p.kv.n_kv + j) * (page_mask + 1) + (key & page_mask);
         raw_s = live ? (g ? p.kv.sv : p.kv.sk)[a] : 0.0f;
       }
     }
   };
-  // INT8: the staged codes into buffer b as bf16
+  // INT8: the staged codes into buffer b as bf16, the scales into set t % 4 (keys) or
+  // (t - 1) % 4 (values, one tile behind)
   auto put = [&](int b, int v) {
     if constexpr (I8) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-          const int idx = 64 * i + here(l), r = idx / (ROWG / 16), c = idx % (ROWG / 16);
-          const v4i u = raw[i];
-          const uint32_t x[4] = {(uint32_t)u.x, (uint32_t)u.y, (uint32_t)u.z, (uint32_t)u.w};
-          uint32_t o[8];
+      for (int i = 0; i < LOADS; ++i) {
+        const int idx = 64 * i + here(l), r = idx / (ROWG / 16), c = idx % (ROWG / 16);
+        const v4i u = raw[v * LOADS + i];
+        const uint32_t x[4] = {(uint32_t)u.x, (uint32_t)u.y, (uint32_t)u.z, (uint32_t)u.w};
+        uint32_t o[8];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            o[2 * e] = (uint32_t)pair_hi(byte_f(x[e], 0), byte_f(x[e], 1));
-            o[2 * e + 1] = (uint32_t)pair_hi(byte_f(x[e], 2), byte_f(x[e], 3));
-          }
-          char* dst = mine + (2 * b + v) * TILEB + (8 * rg + r) * ROWL;
-          const int z = swizzle(8 * rg + r, v);
-          *reinterpret_cast<uint4*>(dst + 16 * ((2 * c) ^ z)) = make_uint4(o[0], o[1], o[2], o[3]);
-          *reinterpret_cast<uint4*>(dst + 16 * ((2 * c + 1) ^ z)) = make_uint4(o[4], o[5], o[6], o[7]);
+        for (int e = 0; e < 4; ++e) {
+          o[2 * e] = (uint32_t)pair_hi(byte_f(x[e], 0), byte_f(x[e], 1));
+          o[2 * e + 1] = (uint32_t)pair_hi(byte_f(x[e], 2), byte_f(x[e], 3));
         }
-      if (rg == 0 && v == 0) scales[(kg * 2 + b) * 64 + l] = raw_s;
+        char* dst = mine + (2 * b + v) * TILEB + (8 * rg + r) * ROWL;
+        const int z = swizzle(8 * rg + r, v);
+        *reinterpret_cast<uint4*>(dst + 16 * ((2 * c) ^ z)) = make_uint4(o[0], o[1], o[2], o[3]);
+        *reinterpret_cast<uint4*>(dst + 16 * ((2 * c + 1) ^ z)) = make_uint4(o[4], o[5], o[6], o[7]);
+      }
+    }
+  };
+  auto put_scales = [&](int tk, int tv) {
+    if constexpr (I8) {
+      if (rg == 0) scales[(kg * 4 + ((g ? tv : tk) & 3)) * 64 + l] = raw_s;
     }
   };
 
@@ -583,25 +597,57 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
   const int voff = TILEB + vr * ROWL + 8 * (l & 1) + 16 * (2 * ((l >> 4) & 1) + ((l >> 1) & 1)) + 64 * (vr & 3);
 
   // h0, h1: the two pages held; whole: every row attends every key
-  v4i pw[2];  // the weights of a tile
-  auto weights = [&](int k0, int b, bool h0, bool h1, bool whole) {
-    const char* buf = mine + 2 * b * TILEB;
-    v16f s;
+  v16f s;     // a tile's scores
+  v4i pw[2];  // a tile's weights
+  auto key_frag = [&](const char* buf, int ko, int c) {
+    return *reinterpret_cast<const v4i*>(buf + (ko ^ (32 * (c & 7))) + 256 * (c >> 3));
+  };
+  auto value_frag = [&](const char* buf, int vo, int u) {
+    const int h = u / NB, i = u % NB;
+    const char* a = buf + (vo ^ (64 * (i & 3))) + 16 * h * ROWL + 256 * (i >> 2);
+    typedef __attribute__((address_space(3))) v4s* lds4;
+    const v4s lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)a), hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(a + 8 * ROWL));
+    const int2 x = __builtin_bit_cast(int2, lo4), y = __builtin_bit_cast(int2, hi4);
+    return v4i{x.x, x.y, y.x, y.y};
+  };
+  // Matrix products: scores of the tile in key buffer kb and, do_v, the value product
+  // of the weights with value buffer vb, in turn (the scores are one chain, whose
+  // latency the others fill); the reads of LDS some products ahead.  One form for all
+  // tiles of the loop, seen or not (weights of 0): with a branch around the
+  // products the compiler moves the 128 output registers about.
+  auto products = [&](auto do_s, auto do_v, int kb, int vb) {
+    constexpr bool DS = decltype(do_s)::value, DV = decltype(do_v)::value;
+    constexpr int AH = DS && DV ? 2 : 3;
+    static_assert(NC == 2 * NB, "as many products either way");
+    const char* kbuf = mine + 2 * kb * TILEB;
+    const char* vbuf = mine + 2 * vb * TILEB;
+    const int ko = here(koff), vo = here(voff);
+    v4i kf[AH], vf[AH];
+    if constexpr (DS) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+      for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+    }
     __builtin_amdgcn_sched_barrier(0);
-    v4i kf[kAhead];
-    const int ko = here(koff);
 #pragma unroll
-    for (int c = 0; c < NC + kAhead; ++c) {  // the reads of kAhead products ahead
-      if (c >= kAhead) s = mma32_bf16(kf[c % kAhead], q[c - kAhead], s);
-      if (c < NC) kf[c % kAhead] = *reinterpret_cast<const v4i*>(buf + (ko ^ (32 * (c & 7))) + 256 * (c >> 3));
+    for (int t = 0; t < NC + AH; ++t) {
+      const int u = t - AH;
+      if (u >= 0) {
+        if constexpr (DS) s = mma32_bf16(kf[u % AH], q[u], s);
+        if constexpr (DV) acc[u % NB] = mma32_bf16(vf[u % AH], pw[u / NB], acc[u % NB]);
+      }
+      if (t < NC) {
+        if constexpr (DS) kf[t % AH] = key_frag(kbuf, ko, t);
+        if constexpr (DV) vf[t % AH] = value_frag(vbuf, vo, t);
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
-    const float* sc = scales + (kg * 2 + b) * 64 + 4 * g;
+  };
+  // Scores to weights.  h0, h1: the two pages held; whole: every row attends every key.
+  auto weights = [&](int k0, int t, bool h0, bool h1, bool whole) {
+    const float* sc = scales + (kg * 4 + (t & 3)) * 64 + 4 * g;
     float x[16];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] = s[r] * p.scale_log2;
+    for (int r = 0; r < 16; ++r) x[r] = s[r];
     if constexpr (I8) {
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
@@ -619,7 +665,7 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
     float mx = x[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
-    mx = max32(mx);
+    mx = max32(mx) * scale;
     if (__any(mx > ref + 8.0f)) {
       const float next = fmaxf(ref, mx), corr = next == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - next);
       ref = next;
@@ -632,7 +678,7 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
     const float m = ref == -INFINITY ? 0.0f : ref;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      x[r] = __builtin_amdgcn_exp2f(x[r] - m);
+      x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], scale, -m));
       sum += x[r];
     }
     if constexpr (I8) {
@@ -647,60 +693,69 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
       pw[h] = v4i{(int)pack2(x[8 * h], x[8 * h + 1]), (int)pack2(x[8 * h + 2], x[8 * h + 3]),
                   (int)pack2(x[8 * h + 4], x[8 * h + 5]), (int)pack2(x[8 * h + 6], x[8 * h + 7])};
   };
-  auto values = [&](int b) {
-    const char* buf = mine + 2 * b * TILEB;
+  auto sync = []() {
     __builtin_amdgcn_sched_barrier(0);
-    v4i vf[kAhead];
-    const int vo = here(voff);
-#pragma unroll
-    for (int t = 0; t < 2 * NB + kAhead; ++t) {
-      const int u = t - kAhead;
-      if (u >= 0) acc[u % NB] = mma32_bf16(vf[u % kAhead], pw[u / NB], acc[u % NB]);
-      if (t < 2 * NB) {
-        const int h = t / NB, i = t % NB;
-        const char* a = buf + (vo ^ (64 * (i & 3))) + 16 * h * ROWL + 256 * (i >> 2);
-        typedef __attribute__((address_space(3))) v4s* lds4;
-        const v4s lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)a), hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(a + 8 * ROWL));
-        const int2 x = __builtin_bit_cast(int2, lo4), y = __builtin_bit_cast(int2, hi4);
-        vf[t % kAhead] = v4i{x.x, x.y, y.x, y.y};
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+    __builtin_amdgcn_sched_barrier(0);
   };
 
+  // The two key groups' waves of a row group share a SIMD, half a tile apart: while
+  // one is in its matrix products (values of a tile with scores of the next), the
+  // other forms weights and sends for the tiles to come, so that matrix and vector
+  // units work at the same time.  Tile t's keys and values are in the buffers t % 2; the
+  // keys of t + 2 and the values of t + 1 are sent for as soon as those of t and t - 1
+  // have been used.
   const int n_it = (hi - begin + 2 * kStep - 1) / (2 * kStep);
-  find(begin + kStep * kg);
-  stage(begin + kStep * kg, 0, 0);
+  const int key0 = begin + kStep * kg;
+  auto sees = [&](int k0, Pages pg) {
+    return any && k0 <= pos1 && k0 < hi && k0 + kStep > pos0 + 1 - p.window && max(pg.a, pg.b) >= 0;
+  };
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+  Pages pg0 = pages(key0), pg1 = pages(key0 + 2 * kStep), pg2 = pages(key0 + 4 * kStep);
+  stage(key0, pg0, 0, 0);
+  stage(key0, pg0, 0, 1);
+  stage_scales(key0, pg0, key0, pg0);
   put(0, 0);
-  stage(begin + kStep * kg, 0, 1);
   put(0, 1);
-  find(begin + kStep * (kg + 2));
-  for (int it = 0; it < n_it; ++it) {
-    const int k0 = begin + kStep * (2 * it + kg), b = it & 1;
-    const bool now0 = held0, now1 = held1;
-    __builtin_amdgcn_s_waitcnt((15 << 8) | (7 << 4));  // this wave's loads into LDS
-    __syncthreads();
-    // the next tile: bf16 straight into LDS; INT8 through the same registers, the
-    // keys while the scores are formed, the values during the value product
-    if constexpr (I8) {
-      stage(k0 + 2 * kStep, b ^ 1, 0);  // past the end: page 0, for nothing
-    } else if (it + 1 < n_it) {
-      stage(k0 + 2 * kStep, b ^ 1, 0);
-      stage(k0 + 2 * kStep, b ^ 1, 1);
-    }
-    const bool seen = any && k0 <= pos1 && k0 < hi && k0 + kStep > pos0 + 1 - p.window && (now0 || now1);
-    if (seen) weights(k0, b, now0, now1, now0 && now1 && k0 + kStep - 1 <= pos0 && k0 > pos1 - p.window && k0 + kStep <= hi);
-    if constexpr (I8) {
-      put(b ^ 1, 0);
-      stage(k0 + 2 * kStep, b ^ 1, 1);
-    }
-    if (seen) values(b);
-    find(k0 + 4 * kStep);
-    put(b ^ 1, 1);
+  put_scales(0, 0);
+  stage(key0 + 2 * kStep, pg1, 1, 0);
+  stage_scales(key0 + 2 * kStep, pg1, key0, pg0);
+  put(1, 0);
+  put_scales(1, 0);
+  __builtin_amdgcn_s_waitcnt((15 << 8) | (7 << 4));
+  sync();
+  if (kg == 1) sync();
+  products(yes, no, 0, 0);
+  for (int t = 0; t < n_it; ++t) {
+    const int k0 = key0 + 2 * kStep * t;
+    sync();
+    const Pages pg3 = pages(k0 + 6 * kStep);  // here, so that the wait at the step's end finds it done
+    stage(k0 + 4 * kStep, pg2, t & 1, 0);  // past the end: zeros, so that there are as many loads
+    stage(k0 + 2 * kStep, pg1, (t + 1) & 1, 1);
+    stage_scales(k0 + 4 * kStep, pg2, k0 + 2 * kStep, pg1);
+    if (sees(k0, pg0))
+      weights(k0, t, pg0.a >= 0, pg0.b >= 0, min(pg0.a, pg0.b) >= 0 && k0 + kStep - 1 <= pos0 && k0 > pos1 - p.window && k0 + kStep <= hi);
+    else
+      pw[0] = pw[1] = v4i{0, 0, 0, 0};
+    put(t & 1, 0);
+    put((t + 1) & 1, 1);
+    put_scales(t + 2, t + 1);
+    pg0 = pg1;
+    pg1 = pg2;
+    pg2 = pg3;
+    // the loads before this step's
+    if constexpr (!I8) __builtin_amdgcn_s_waitcnt(((2 * LOADS) & 15) | (7 << 4) | (15 << 8));
+    sync();
+    __builtin_amdgcn_s_setprio(1);
+    products(yes, yes, (t + 1) & 1, t & 1);  // behind the last tile: scores that nobody uses
+    __builtin_amdgcn_s_setprio(0);
   }
+  if (kg == 0) sync();
 
   // ---- the two key groups
   sum = sum32(sum);
+  __builtin_amdgcn_s_waitcnt((15 << 8) | (7 << 4));  // the last loads into LDS, which takes the outputs now
   __syncthreads();
   int lane = threadIdx.x;  // from here on: what the loop need not hold registers for
   asm volatile("" : "+v"(lane));
@@ -830,7 +885,7 @@ size_t attn_paged_ws_bytes(const PagedAttnParams& p, int head_dim) {
 
 template <int D, bool I8>
 static hipError_t tile_launch(const PagedAttnParams& p, hipStream_t st) {
-  constexpr int kLds = 8 * kStep * 2 * D + 1024;
+  constexpr int kLds = 8 * kStep * 2 * D + 2048;
   auto kern = attn_tile_kernel<D, I8>;
   if constexpr (kLds > 64 * 1024) {
     static bool attr_set[64] = {};  // by device; benign race: every caller sets the same value
