@@ -521,8 +521,8 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
     return id < p.kv.n_pages ? max(id, -1) : -1;
   };
   auto pages = [&](int k0) { return Pages{page_at(k0), page_at(k0 + 16)}; };
-  // The wave's 8 rows of the tile at k0 (they lie in one page) on their way to buffer
-  // b: keys (v = 0), values (v = 1).
+  // The wave's 8 rows of the tile at k0 (they lie in one page) on their way: keys
+  // (v = 0), values (v = 1), bf16 straight to buffer b.
   auto stage = [&](int k0, Pages pg, int b, int v) {
     const int id = rg >= 2 ? pg.b : pg.a, key = k0 + 8 * rg;
     const int64_t at = (((int64_t)max(id, 0) * p.kv.n_kv + j) << p.kv.page_log2) + (key & page_mask);
@@ -537,9 +537,10 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
     } else {
 #pragma unroll 1
       for (int i = 0; i < LOADS; ++i) {
-        const int idx = 64 * i + l, r = idx / kChunks, c = idx % kChunks;
-        const GlobalVec src = id >= 0 && key + r >= lo && key + r < hi ? (GlobalVec)(base + r * ROWG + 16 * (c ^ swizzle(8 * rg + r, v))) : (GlobalVec)&kZeros;
-        load_lds16(src, lds0 + (2 * b + v) * TILEB + 1024 * i);
+        const int idx = 64 * i + here(l), r = idx / kChunks, c = idx % kChunks;
+        uint64_t src = (uint64_t)(uintptr_t)(base + r * ROWG + 16 * (c ^ swizzle(8 * rg + r, v)));
+        src = id >= 0 && key + r >= lo && key + r < hi ? src : (uint64_t)(uintptr_t)&kZeros;
+        load_lds16((GlobalVec)(uintptr_t)src, lds0 + (2 * b + v) * TILEB + 1024 * i);
       }
     }
   };
@@ -727,13 +728,20 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
   sync();
   if (kg == 1) sync();
   products(yes, no, 0, 0);
+  if constexpr (I8) {  // the codes go through registers, half a step earlier
+    stage(key0 + 4 * kStep, pg2, 0, 0);
+    stage(key0 + 2 * kStep, pg1, 1, 1);
+    stage_scales(key0 + 4 * kStep, pg2, key0 + 2 * kStep, pg1);
+  }
   for (int t = 0; t < n_it; ++t) {
     const int k0 = key0 + 2 * kStep * t;
     sync();
+    // weights of tile t
     const Pages pg3 = pages(k0 + 6 * kStep);  // here, so that the wait at the step's end finds it done
-    stage(k0 + 4 * kStep, pg2, t & 1, 0);  // past the end: zeros, so that there are as many loads
-    stage(k0 + 2 * kStep, pg1, (t + 1) & 1, 1);
-    stage_scales(k0 + 4 * kStep, pg2, k0 + 2 * kStep, pg1);
+    if constexpr (!I8) {  // past the end: zeros, so that there are as many loads
+      stage(k0 + 4 * kStep, pg2, t & 1, 0);
+      stage(k0 + 2 * kStep, pg1, (t + 1) & 1, 1);
+    }
     if (sees(k0, pg0))
       weights(k0, t, pg0.a >= 0, pg0.b >= 0, min(pg0.a, pg0.b) >= 0 && k0 + kStep - 1 <= pos0 && k0 > pos1 - p.window && k0 + kStep <= hi);
     else
@@ -741,15 +749,21 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
     put(t & 1, 0);
     put((t + 1) & 1, 1);
     put_scales(t + 2, t + 1);
-    pg0 = pg1;
-    pg1 = pg2;
-    pg2 = pg3;
     // the loads before this step's
     if constexpr (!I8) __builtin_amdgcn_s_waitcnt(((2 * LOADS) & 15) | (7 << 4) | (15 << 8));
     sync();
+    // values of tile t, scores of tile t + 1 (behind the last: scores that nobody uses)
     __builtin_amdgcn_s_setprio(1);
-    products(yes, yes, (t + 1) & 1, t & 1);  // behind the last tile: scores that nobody uses
+    products(yes, yes, (t + 1) & 1, t & 1);
     __builtin_amdgcn_s_setprio(0);
+    if constexpr (I8) {  // into registers while the last products are on, for the next step to put
+      stage(k0 + 6 * kStep, pg3, (t + 1) & 1, 0);
+      stage(k0 + 4 * kStep, pg2, t & 1, 1);
+      stage_scales(k0 + 6 * kStep, pg3, k0 + 4 * kStep, pg2);
+    }
+    pg0 = pg1;
+    pg1 = pg2;
+    pg2 = pg3;
   }
   if (kg == 0) sync();
 
