@@ -51,10 +51,17 @@ __device__ __forceinline__ float value_of(uint32_t key) {
   return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
 
+// 16 bytes of a row, which need not lie at a multiple of 16 (f32 rows of odd length do not):
+// the loads take any address.  Logit by logit 131 such rows of 100003 took 44 us to scan,
+// not 28, and 87 to draw from, not 44.
+typedef uint32_t Four __attribute__((ext_vector_type(4)));
+typedef Four Four32 __attribute__((aligned(4)));
+typedef Four Four16 __attribute__((aligned(2)));
+
 struct Row {
   const void* base;
   int64_t n;
-  bool bf, wide;  // wide: 16-byte loads
+  bool bf;
   uint32_t top;   // key of the largest logit
   double best, inv_t;
 };
@@ -67,18 +74,16 @@ __device__ __forceinline__ uint32_t key_at(const Row& r, int64_t i) {
 
 // the keys of eight logits from index i on (a multiple of 8); 0 behind the row
 __device__ __forceinline__ void keys8(const Row& r, int64_t i, uint32_t (&k)[kVec]) {
-  if (r.wide && i + kVec <= r.n) {
+  if (i + kVec <= r.n) {
     if (r.bf) {
-      const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(r.base) + i);
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+      const Four w = *reinterpret_cast<const Four16*>(reinterpret_cast<const uint16_t*>(r.base) + i);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) k[e] = key_of(bf16_bits_to_float((w[e >> 1] >> (16 * (e & 1))) & 0xffffu));
     } else {
-      const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(r.base) + i);
-      const float4 a = p[0], b = p[1];
-      const float f[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+      const Four32* p = reinterpret_cast<const Four32*>(reinterpret_cast<const float*>(r.base) + i);
+      const Four a = p[0], b = p[1];
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) k[e] = key_of(f[e]);
+      for (int e = 0; e < kVec; ++e) k[e] = key_of(__uint_as_float(e < 4 ? a[e] : b[e - 4]));
     }
   } else {
 #pragma unroll
@@ -308,7 +313,6 @@ __device__ __forceinline__ Row row_of(const SampleParams& p, int64_t row, bool b
   r.n = p.n;
   r.base = bf ? (const void*)(reinterpret_cast<const uint16_t*>(p.logits) + row * p.ld)
               : (const void*)(reinterpret_cast<const float*>(p.logits) + row * p.ld);
-  r.wide = (reinterpret_cast<uintptr_t>(r.base) & 15u) == 0;
   return r;
 }
 
@@ -457,47 +461,41 @@ template <bool BF>
 struct Vec;
 template <>
 struct Vec<true> {
-  uint4 a;
+  Four a;
   __device__ __forceinline__ uint32_t bits(int e) const {  // of the binary32 value
-    const uint32_t w = e < 2 ? a.x : e < 4 ? a.y : e < 6 ? a.z : a.w;
-    return e & 1 ? w & 0xffff0000u : w << 16;
+    return e & 1 ? a[e >> 1] & 0xffff0000u : a[e >> 1] << 16;
   }
   __device__ __forceinline__ void load(const Row& r, int64_t i) {
     const uint16_t* p = reinterpret_cast<const uint16_t*>(r.base) + i;
-    if (r.wide && i + 8 <= r.n) {
-      a = *reinterpret_cast<const uint4*>(p);
+    if (i + 8 <= r.n) {
+      a = *reinterpret_cast<const Four16*>(p);
     } else {
-      uint32_t w[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e)  // NaN behind the row
-        w[e] = (i + 2 * e < r.n ? p[2 * e] : 0x7fffu) | ((i + 2 * e + 1 < r.n ? p[2 * e + 1] : 0x7fffu) << 16);
-      a = make_uint4(w[0], w[1], w[2], w[3]);
+        a[e] = (i + 2 * e < r.n ? p[2 * e] : 0x7fffu) | ((i + 2 * e + 1 < r.n ? p[2 * e + 1] : 0x7fffu) << 16);
     }
   }
 };
 template <>
 struct Vec<false> {
-  float4 a, b;
-  __device__ __forceinline__ uint32_t bits(int e) const {
-    return __float_as_uint(e == 0 ? a.x : e == 1 ? a.y : e == 2 ? a.z : e == 3 ? a.w : e == 4 ? b.x : e == 5 ? b.y : e == 6 ? b.z : b.w);
-  }
+  Four a, b;
+  __device__ __forceinline__ uint32_t bits(int e) const { return e < 4 ? a[e] : b[e - 4]; }
   __device__ __forceinline__ void load(const Row& r, int64_t i) {
     const float* p = reinterpret_cast<const float*>(r.base) + i;
-    if (r.wide && i + 8 <= r.n) {
-      a = reinterpret_cast<const float4*>(p)[0];
-      b = reinterpret_cast<const float4*>(p)[1];
+    if (i + 8 <= r.n) {
+      a = reinterpret_cast<const Four32*>(p)[0];
+      b = reinterpret_cast<const Four32*>(p)[1];
     } else {
-      float f[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = i + e < r.n ? p[e] : NAN;
-      a = make_float4(f[0], f[1], f[2], f[3]);
-      b = make_float4(f[4], f[5], f[6], f[7]);
+      for (int e = 0; e < 8; ++e) (e < 4 ? a : b)[e & 3] = __float_as_uint(i + e < r.n ? p[e] : NAN);
     }
   }
 };
 
+// registers: four workgroups a CU for f32 (all of 131 x 100003 logits at once: 28 us); bf16 spills
+// with as few, and 64 x 262144 logits take 28 us instead of 25
 template <bool BF>
-__global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(SampleParams p, ChunkWs ws) {
+__global__ __launch_bounds__(kScanThreads, BF ? 4 : 8) void sample_scan_kernel(SampleParams p, ChunkWs ws) {
   constexpr int V = kChunk / kScanThreads / kVec, kFixed = BF ? 2 * kBand : kBins;
   static_assert(V * kVec == 32, "a bit of a word for each logit of a thread");
   __shared__ uint32_t hist[kBins];
@@ -624,10 +622,22 @@ union DrawUnion {
 };
 
 // The m logits of bin b of a row into s.list, in order.  A call, like exp_call:
-// five places need it, none of them in every row.
+// five places need it, none of them in every row.  One workgroup reads the row, and
+// what it does for each logit bounds that (48 us of 262144 when it formed the bin of
+// each), so a logit's bits are compared with the range that the bin is of them.
+template <bool BF>
 __device__ __attribute__((noinline)) void gather_bin(const Row& r, DrawLds& s, const uint16_t* count, int C, int first, int b, uint32_t m) {
   const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6;
   constexpr int kWaves = kThreads / kWave, kParts = 8;  // parts of a chunk, so that few chunks occupy all waves
+  constexpr int kLoads = kChunk / kParts / (kWave * kVec);
+  // the bin's magnitudes, upper 16 bits: [m0, m1); of the infinities no NaN
+  const int place = first - b, x = place < 0 ? ~place : place;
+  const uint32_t m0 = x < kBand ? __float_as_uint((float)x * (1.0f / 256.0f)) >> 16 : (uint32_t)(x - kBand) + kBandBits;
+  const uint32_t m1 = x < kBand ? __float_as_uint((float)(x + 1) * (1.0f / 256.0f)) >> 16 : m0 + 1;
+  const uint32_t sign = place < 0 ? 0x80000000u : 0u;
+  const uint32_t lo = sign | (m0 << 16) | (place == -1 ? 1u : 0u);  // -0 is 0, of place 0
+  const uint32_t span = m0 == 0x7f80u ? 1u : (sign | (m1 << 16)) - lo;
+  const bool zero = place == 0;
   __syncthreads();
   if (tid == 0) s.n = 0;
   for (int i = tid; i < kList; i += kThreads) s.list[i] = ~0ull;
@@ -635,18 +645,32 @@ __device__ __attribute__((noinline)) void gather_bin(const Row& r, DrawLds& s, c
   for (int cp = wave; cp < C * kParts; cp += kWaves) {
     const int c = cp / kParts, d = b - s.off[c];
     if (d < 0 || !count[(int64_t)c * kBins + d]) continue;
-    const int64_t at0 = (int64_t)c * kChunk + (cp % kParts) * (kChunk / kParts);
+    const int64_t at0 = (int64_t)c * kChunk + (cp % kParts) * (kChunk / kParts) + lane * kVec;
+    Vec<BF> y[kLoads];
 #pragma unroll
-    for (int v = 0; v < kChunk / kParts / (kWave * kVec); ++v) {
-      const int64_t i = at0 + (v * kWave + lane) * kVec;
-      uint32_t k[kVec];
-      keys8(r, i, k);
+    for (int v = 0; v < kLoads; ++v) y[v].load(r, at0 + v * kWave * kVec);  // NaN behind the row
 #pragma unroll
-      for (int e = 0; e < kVec; ++e)
-        if (k[e] && first - place_of(k[e]) == b) {
-          const int at = atomicAdd(&s.n, 1);
-          if (at < kList) s.list[at] = ((unsigned long long)~k[e] << 32) | (unsigned long long)(i + e);
-        }
+    for (int v = 0; v < kLoads; ++v) {
+      uint32_t hits = 0;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) hits |= y[v].bits(e) - lo < span ? 1u << e : 0u;
+      if (zero) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) hits |= y[v].bits(e) == 0x80000000u ? 1u << e : 0u;
+      }
+      if (hits) {
+        int at = atomicAdd(&s.n, __popc(hits));
+        do {
+          const int e = __builtin_ctz(hits);
+          hits &= hits - 1;
+          uint32_t bits = y[v].bits(0);
+#pragma unroll
+          for (int f = 1; f < kVec; ++f) bits = e == f ? y[v].bits(f) : bits;
+          if (at < kList)
+            s.list[at] = ((unsigned long long)~key_of(__uint_as_float(bits)) << 32) | (unsigned long long)(at0 + v * kWave * kVec + e);
+          ++at;
+        } while (hits);
+      }
     }
   }
   __syncthreads();
@@ -662,8 +686,16 @@ __device__ __attribute__((noinline)) void gather_bin(const Row& r, DrawLds& s, c
           s.list[j] = x;
         }
       }
-      __syncthreads();
+      // the 64 pairs of a wave are of 128 neighbours where step <= 64, and a wave's LDS accesses
+      // are in order: 10 of 66 steps of 2048 logits need the workgroup's barrier
+      if (max(step, step > 1 ? step / 2 : len) > kWave) {
+        __syncthreads();
+      } else {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      }
     }
+  __syncthreads();
 }
 
 template <bool BF>
@@ -684,6 +716,14 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p, C
     const uint32_t* src = reinterpret_cast<const uint32_t*>(count + (int64_t)c * kBins) + lane;
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) v[i] = 2 * kWave * i < end ? src[kWave * i] : 0u;
+  };
+  // f32: the weights of kAhead pairs of them, all loads before the first use (3 of
+  // 90 us of 131 rows of 100003)
+  constexpr int kAhead = 8;
+  auto load_fixed = [&](int c, int i0, int end, ulonglong2(&v)[kAhead]) {
+    const ulonglong2* src = reinterpret_cast<const ulonglong2*>(fix + (int64_t)c * kFixed) + lane;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) v[i] = 2 * kWave * (i0 + i) < end ? src[kWave * (i0 + i)] : ulonglong2{0, 0};
   };
   uint32_t q[kPairs];
   if (wave < C) load_counts(wave, kBins, q);
@@ -734,15 +774,19 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p, C
       if (f) atomicAdd(&s.f_bin[lane], (unsigned long long)rint((double)f * scale));
     }
 #pragma unroll
-    for (int i = 0; i < kPairs; ++i) {
-      const int d = 2 * (kWave * i + lane), b = d + off;
-      const uint32_t m0 = q[i] & 0xffffu, m1 = q[i] >> 16;
-      if (m0 && b < kBins - 1) atomicAdd(&s.n_bin[b], m0);
-      if (m1 && b + 1 < kBins - 1) atomicAdd(&s.n_bin[b + 1], m1);
-      if constexpr (!BF) {
-        const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(fix + (int64_t)c * kFixed + d);
-        if (f.x && b < kBins - 1) atomicAdd(&s.f_bin[b], (unsigned long long)rint((double)f.x * scale));
-        if (f.y && b + 1 < kBins - 1) atomicAdd(&s.f_bin[b + 1], (unsigned long long)rint((double)f.y * scale));
+    for (int i0 = 0; i0 < kPairs; i0 += kAhead) {
+      ulonglong2 f[kAhead];
+      if constexpr (!BF) load_fixed(c, i0, kBins, f);
+#pragma unroll
+      for (int i = i0; i < i0 + kAhead; ++i) {
+        const int b = 2 * (kWave * i + lane) + off;
+        const uint32_t m0 = q[i] & 0xffffu, m1 = q[i] >> 16;
+        if (m0 && b < kBins - 1) atomicAdd(&s.n_bin[b], m0);
+        if (m1 && b + 1 < kBins - 1) atomicAdd(&s.n_bin[b + 1], m1);
+        if constexpr (!BF) {
+          if (f[i - i0].x && b < kBins - 1) atomicAdd(&s.f_bin[b], (unsigned long long)rint((double)f[i - i0].x * scale));
+          if (f[i - i0].y && b + 1 < kBins - 1) atomicAdd(&s.f_bin[b + 1], (unsigned long long)rint((double)f[i - i0].y * scale));
+        }
       }
     }
   }
@@ -791,7 +835,7 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p, C
   bool lost = false;
   // the logits of bin b (m of them) into the list, in order
   auto gather = [&](int b, uint32_t m) {
-    if (listed != b) gather_bin(r, s, count, C, first, b, m);
+    if (listed != b) gather_bin<BF>(r, s, count, C, first, b, m);
     listed = b;
   };
   auto list_weight = [&](int i) { return weight_call(r, ~(uint32_t)(s.list[i] >> 32)); };
@@ -948,15 +992,31 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p, C
     const int off = s.off[c];
     double x = 0.0;
     const int end = a.greedy ? 0 : min(bin, kBins - 1) - off;
-    load_counts(c, end, q);
+    if constexpr (BF) {
+      load_counts(c, end, q);
+      const int d = first - (lane - kBand) - off;  // the lane's bin of the band
+      if (d >= 0 && d < end) x = fixed_sum(c, d + off);
 #pragma unroll
-    for (int i = 0; i < kPairs; ++i)
+      for (int i = 0; i < kPairs; ++i)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint32_t m = e ? q[i] >> 16 : q[i] & 0xffffu;
-        const int d = 2 * (kWave * i + lane) + e;
-        if (m && d < end) x += one_value(d + off) ? (double)m * s.w[d + off] : fixed_sum(c, d + off);
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t m = e ? q[i] >> 16 : q[i] & 0xffffu;
+          const int d = 2 * (kWave * i + lane) + e;
+          if (m && d < end && one_value(d + off)) x += (double)m * s.w[d + off];
+        }
+    } else {
+#pragma unroll
+      for (int i0 = 0; i0 < kPairs; i0 += kAhead) {
+        ulonglong2 f[kAhead];
+        load_fixed(c, i0, end, f);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          const int d = 2 * (kWave * (i0 + i) + lane);
+          if (d < end) x += (double)f[i].x * s.scale[c];
+          if (d + 1 < end) x += (double)f[i].y * s.scale[c];
+        }
       }
+    }
     if (bin < kBins - 1 && kept > 0) {
       if (single) {
         if (lane == 0) x += (double)s.ties[c] * tie_weight;

@@ -820,17 +820,18 @@ class _on:
         self.device, self.stream = device, stream
 
     def __enter__(self):
-        self.old = torch.cuda.current_device()
-        if self.device.index != self.old:
+        index = self.device.index
+        self.ctx, self.old = None, torch.cuda.current_device()
+        if index != self.old:
             torch.cuda.set_device(self.device)
-        self.ctx = None
-        if self.stream is not None:
-            if self.stream.device != self.device:
-                self.__exit__()
-                raise ValueError("the stream is not on the tensors' device")
-            self.ctx = torch.cuda.stream(self.stream)
-            self.ctx.__enter__()
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        if self.stream is None:  # its handle without a stream object, which takes 2 us to make
+            return torch._C._cuda_getCurrentRawStream(index)
+        if self.stream.device != self.device:
+            self.__exit__()
+            raise ValueError("the stream is not on the tensors' device")
+        self.ctx = torch.cuda.stream(self.stream)
+        self.ctx.__enter__()
+        return self.stream.cuda_stream
 
     def __exit__(self, *exc):
         if self.ctx is not None:
@@ -843,16 +844,19 @@ def _need(t, name, dtype, device, shape=None):
     """t as an argument: a contiguous GPU tensor of a type, on a device, of a shape."""
     if not isinstance(t, torch.Tensor) or t.device != device or t.dtype != dtype:
         raise ValueError("%s must be a %s tensor on %s" % (name, dtype, device))
-    if not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+    if not t.is_contiguous() or (shape is not None and t.shape != shape):
         raise ValueError("%s must be contiguous%s" % (name, "" if shape is None else " of shape %s" % (tuple(shape),)))
     return t
 
 
 def _row_stride(x, name):
     """Elements from row to row of a [rows, heads, d] tensor whose rows are dense."""
-    if x.dim() != 3 or not x.is_cuda or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]):
+    if x.dim() != 3 or not x.is_cuda:
         raise ValueError("%s must be a GPU tensor [rows, heads, head_dim] with dense rows" % name)
-    return x.stride(0) if x.shape[0] > 1 else -(-x.shape[1] * x.shape[2] // 8) * 8
+    (rows, heads, d), (row, head, one) = x.shape, x.stride()
+    if one != 1 or (heads > 1 and head != d):
+        raise ValueError("%s must be a GPU tensor [rows, heads, head_dim] with dense rows" % name)
+    return row if rows > 1 else -(-heads * d // 8) * 8
 
 
 @dataclass
