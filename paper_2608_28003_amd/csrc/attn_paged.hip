@@ -25,6 +25,7 @@ namespace {
 constexpr int kStep = 32;          // keys a wave takes at a time
 constexpr int kPass = 4 * kStep;   // ... and a workgroup
 constexpr int kRows = 16;          // rows of the row-tile kernel
+constexpr int kSplitSeqs = 512;    // sequences that the row kernel's workgroups share out among them
 
 // INT8 code e of a word (exact in bf16)
 __device__ __forceinline__ float byte_f(uint32_t w, int e) {
@@ -46,15 +47,19 @@ struct Seq {
   int q0, q_len;
   int first;  // position of the first new token
 };
-__device__ __forceinline__ bool seq_of(const PagedAttnParams& p, int s, Seq* t) {
-  const ConstInts start = (ConstInts)p.batch.q_start;
-  const int q0 = start[s], q1 = start[s + 1];
+__device__ __forceinline__ bool seq_at(const PagedAttnParams& p, int q0, int q1, int ctx, Seq* t) {
   if (q0 < 0 || q1 > p.rows || q1 <= q0 || q1 - q0 > p.max_q) return false;
   t->q0 = q0;
   t->q_len = q1 - q0;
-  t->first = max(((ConstInts)p.batch.ctx_len)[s], 0) - t->q_len;
+  t->first = max(ctx, 0) - t->q_len;
   return true;
 }
+__device__ __forceinline__ bool seq_of(const PagedAttnParams& p, int s, Seq* t) {  // s: the same for a wave
+  const ConstInts start = (ConstInts)p.batch.q_start;
+  return seq_at(p, start[s], start[s + 1], ((ConstInts)p.batch.ctx_len)[s], t);
+}
+// sum over a wave
+__device__ __forceinline__ uint32_t total(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(v), kWave - 1); }
 
 // Keys [lo, hi) that rows row0 .. row1 of a sequence attend, lo in [0, hi]: no
 // position below leaves 32 bits (first positions from -2^25, windows and tables up
@@ -71,10 +76,82 @@ __device__ __forceinline__ Keys keys_of(const PagedAttnParams& p, const Seq& t, 
   return k;
 }
 
+// Work of the row kernel: a sequence of at most 16 rows, or a piece of its keys.
+//
+// Contexts differ by much and only the GPU knows them, so the pieces are counted here:
+// L passes of 128 keys are the fewest for which all pieces of all sequences, ceil(passes
+// / L) of each, are at most p.row_pieces, what the CUs hold at once; a sequence is then
+// cut evenly.  64 contexts of 600 to 16384 keys (240 MB) took 62 us in pieces of a fixed
+// length, whose workgroups did not all fit and were not evenly spread over the XCDs.
+struct RowWork {
+  Seq t;
+  Keys ks;
+  int seq, piece, slot0;  // keys of a piece, slot of the sequence's first one
+};
+// of a slot, or (slot < 0) of sequence `seq`; false: none
+__device__ __forceinline__ bool row_work(const PagedAttnParams& p, int slot, int seq, RowWork* w) {
+  uint32_t k[kSplitSeqs / kWave], len = 1;
+  int slot0 = seq = slot >= 0 ? slot : seq;
+  uint32_t pieces = 1;
+  if (p.row_pieces) {
+    uint32_t sum = 0;
+#pragma unroll
+    for (int c = 0; c < kSplitSeqs / kWave; ++c) {
+      const int s = c * kWave + lane_id();
+      k[c] = 0;
+      if (s < p.batch.n_seqs) {
+        Seq t;
+        if (seq_at(p, p.batch.q_start[s], p.batch.q_start[s + 1], p.batch.ctx_len[s], &t) && t.q_len * p.group <= p.max_rows)
+          k[c] = (uint32_t)keys_of(p, t, 0, t.q_len * p.group - 1, kPass).pieces;
+      }
+      sum += k[c];
+    }
+    sum = total(sum);
+    const uint32_t slots = (uint32_t)p.row_pieces;
+    len = max((sum + slots - 1) / slots, 1u);
+    for (;;) {  // to the longest at the latest: a piece a sequence, of which there are no more than slots
+      uint32_t n = 0;
+#pragma unroll
+      for (int c = 0; c < kSplitSeqs / kWave; ++c)
+        if (c * kWave < p.batch.n_seqs) n += (k[c] + len - 1) / len;
+      if (total(n) <= slots) break;
+      len += max(len / 16, 1u);
+    }
+    uint32_t before = 0;
+    bool found = false;
+#pragma unroll
+    for (int c = 0; c < kSplitSeqs / kWave; ++c)
+      if (c * kWave < p.batch.n_seqs) {
+        const uint32_t mine = (k[c] + len - 1) / len, upto = before + wave_scan(mine), from = upto - mine;
+        const uint64_t hit = slot >= 0 ? __ballot(from <= (uint32_t)slot && (uint32_t)slot < upto) : seq / kWave == c ? 1ull << (seq % kWave) : 0ull;
+        if (hit && !found) {
+          const int at = __builtin_ctzll(hit);
+          found = true;
+          seq = c * kWave + at;
+          slot0 = __builtin_amdgcn_readlane((int)from, at);
+          pieces = (uint32_t)__builtin_amdgcn_readlane((int)mine, at);
+          len = (uint32_t)__builtin_amdgcn_readlane((int)((k[c] + max(mine, 1u) - 1) / max(mine, 1u)), at);
+          break;
+        }
+        before = (uint32_t)__builtin_amdgcn_readlane((int)upto, kWave - 1);
+      }
+    if (!found || pieces == 0) return false;
+  }
+  seq = __builtin_amdgcn_readfirstlane(seq);
+  if (!seq_of(p, seq, &w->t)) return false;
+  const int rows = w->t.q_len * p.group;
+  if (rows > p.max_rows) return false;
+  w->seq = seq;
+  w->slot0 = __builtin_amdgcn_readfirstlane(slot0);
+  w->piece = p.row_pieces ? __builtin_amdgcn_readfirstlane((int)len) * kPass : 1 << 30;
+  w->ks = keys_of(p, w->t, 0, rows - 1, w->piece);
+  return true;
+}
+
 }  // namespace
 
 // Sequences of at most 16 rows, one a workgroup, and for long contexts a piece of
-// its keys.  Each of the four waves walks every fourth group of 32 keys, straight
+// its keys (row_work).  Each of the four waves walks every fourth group of 32 keys, straight
 // from memory: a lane's pieces of a key row are what lies together in memory (any
 // assignment of the dimensions to the product's K positions serves), and its 16
 // bytes of a value row are one output dimension of sixteen products.  The weights
@@ -83,7 +160,7 @@ __device__ __forceinline__ Keys keys_of(const PagedAttnParams& p, const Seq& t, 
 // held page are read whatever they hold; what no row attends is masked out of the
 // scores, and zeroed in bf16 values (a weight of 0 times NaN).
 template <int D, bool I8>
-__global__ __launch_bounds__(256, I8 ? 2 : 1) void attn_rows_kernel(PagedAttnParams p) {
+__global__ __launch_bounds__(256, 2) void attn_rows_kernel(PagedAttnParams p) {
   constexpr int KI = I8 ? D / 64 : D / 32;  // 16-byte pieces of a lane's quarter of a key row
   constexpr int E = D / 16;                 // dimensions of a lane's part of a value row
   constexpr int VW = I8 ? E / 4 : E / 2;    // ... in words
@@ -92,14 +169,14 @@ __global__ __launch_bounds__(256, I8 ? 2 : 1) void attn_rows_kernel(PagedAttnPar
   __shared__ __attribute__((aligned(16))) float ored[2][kRows][LD];
   __shared__ float om[4][kRows], ol[4][kRows];
 
-  Seq tl;
-  const int seq = blockIdx.x, j = blockIdx.y, split = blockIdx.z;
-  if (!seq_of(p, seq, &tl)) return;  // whole workgroup
-  const int rows = tl.q_len * p.group;
-  if (rows > p.max_rows) return;
-  const Keys ks = keys_of(p, tl, 0, rows - 1, p.piece);
+  RowWork work;
+  const int slot = blockIdx.x, j = blockIdx.y;
+  if (!row_work(p, slot, 0, &work)) return;  // whole workgroup
+  const Seq tl = work.t;
+  const Keys ks = work.ks;
+  const int seq = work.seq, rows = tl.q_len * p.group, split = slot - work.slot0;
   if (split >= ks.pieces) return;
-  const int lo = ks.lo, hi = min(ks.hi, ks.begin + (split + 1) * p.piece);
+  const int begin = ks.begin + split * work.piece, lo = ks.lo, hi = min(ks.hi, begin + min(work.piece, ks.hi - begin));
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = lane_id(), n = l & 15, g = l >> 4;
   const int pos = n < rows ? tl.first + n / p.group : -1;
   const int from = pos < 0 ? 0 : max(0, pos + 1 - p.window);
@@ -155,7 +232,7 @@ __global__ __launch_bounds__(256, I8 ? 2 : 1) void attn_rows_kernel(PagedAttnPar
     }
   };
 
-  int r0 = ks.begin + split * p.piece + kStep * w;
+  int r0 = begin + kStep * w;
   if (r0 < hi) {
     locate(r0);
     load_k();
@@ -280,7 +357,7 @@ __global__ __launch_bounds__(256, I8 ? 2 : 1) void attn_rows_kernel(PagedAttnPar
   const float m = fmaxf(fmaxf(om[0][n], om[1][n]), fmaxf(om[2][n], om[3][n]));
   const float ref = m == -INFINITY ? 0.0f : m;
   const float f = __builtin_amdgcn_exp2f(run_m - ref);
-  auto slot = [&](int r, int e) -> float4& {
+  auto sums = [&](int r, int e) -> float4& {
     return *reinterpret_cast<float4*>(&ored[w & 1][n][E * (4 * g + r) + e]);
   };
   if (w >= 2) {
@@ -288,7 +365,7 @@ __global__ __launch_bounds__(256, I8 ? 2 : 1) void attn_rows_kernel(PagedAttnPar
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int e = 0; e < E; e += 4)
-        slot(r, e) = make_float4(acc[e][r] * f, acc[e + 1][r] * f, acc[e + 2][r] * f, acc[e + 3][r] * f);
+        sums(r, e) = make_float4(acc[e][r] * f, acc[e + 1][r] * f, acc[e + 2][r] * f, acc[e + 3][r] * f);
   }
   __syncthreads();
   if (w < 2) {
@@ -296,12 +373,12 @@ __global__ __launch_bounds__(256, I8 ? 2 : 1) void attn_rows_kernel(PagedAttnPar
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int e = 0; e < E; e += 4) {
-        float4 o = slot(r, e);
+        float4 o = sums(r, e);
         o.x += acc[e][r] * f;
         o.y += acc[e + 1][r] * f;
         o.z += acc[e + 2][r] * f;
         o.w += acc[e + 3][r] * f;
-        slot(r, e) = o;
+        sums(r, e) = o;
       }
   }
   __syncthreads();
@@ -316,7 +393,7 @@ __global__ __launch_bounds__(256, I8 ? 2 : 1) void attn_rows_kernel(PagedAttnPar
 #pragma unroll
     for (int k = 0; k < 8; ++k) x[k] = ored[0][r][d0 + k] + ored[1][r][d0 + k];
     if (ks.pieces > 1) {
-      const int64_t piece = ((int64_t)(seq * p.kv.n_kv + j) * p.max_pieces + split) * p.max_rows + r;
+      const int64_t piece = ((int64_t)j * p.row_pieces + slot) * p.max_rows + r;
       float4* dst = reinterpret_cast<float4*>(p.part + piece * D + d0);
       dst[0] = make_float4(x[0], x[1], x[2], x[3]);
       dst[1] = make_float4(x[4], x[5], x[6], x[7]);
@@ -333,45 +410,57 @@ __global__ __launch_bounds__(256, I8 ? 2 : 1) void attn_rows_kernel(PagedAttnPar
   }
 }
 
-// The pieces of a row: thread (d, i) adds dimension d of the pieces i, i + G, ...
-// (all loads of eight at once), then the groups' sums are added in order.
+// The pieces of a sequence's rows, one workgroup for all of them: D / 4 threads have four
+// dimensions of a row each, and where there are few rows several such groups add
+// every G-th piece; the groups' sums are added in order.
 template <int D>
 __global__ __launch_bounds__(1024) void attn_join_kernel(PagedAttnParams p) {
-  constexpr int G = 1024 / D;
-  __shared__ float red[G][D];
-  Seq tl;
-  const int seq = blockIdx.x, j = blockIdx.y, r = blockIdx.z;
-  if (!seq_of(p, seq, &tl)) return;  // whole workgroup
-  const int rows = tl.q_len * p.group;
-  if (rows > p.max_rows || r >= rows) return;
-  const int pieces = keys_of(p, tl, 0, rows - 1, p.piece).pieces;
+  constexpr int T = D / 4, S = 1024 / T;
+  __shared__ float4 red[S][T];
+  RowWork work;
+  const int j = blockIdx.y;
+  if (!row_work(p, -1, blockIdx.x, &work)) return;  // whole workgroup
+  const int rows = work.t.q_len * p.group, pieces = work.ks.pieces;
   if (pieces == 1) return;  // written already
-  const int64_t base = (int64_t)(seq * p.kv.n_kv + j) * p.max_pieces * p.max_rows + r;
-  const int d = threadIdx.x % D, g = threadIdx.x / D;
-  float m = -INFINITY;
-  for (int i = lane_id(); i < pieces; i += kWave) m = fmaxf(m, p.part_ml[base + (int64_t)i * p.max_rows].x);
-  m = wave_max(m);
+  int G = S;
+  while (G * rows > S) G >>= 1;
+  const int s = threadIdx.x / T, t = threadIdx.x % T, r = s / G, g = s % G;
+  const int64_t base = ((int64_t)j * p.row_pieces + work.slot0) * p.max_rows + min(r, rows - 1);
+  float m = -INFINITY, den = 0.0f;
+  for (int i = t; i < pieces; i += T) m = fmaxf(m, p.part_ml[base + (int64_t)i * p.max_rows].x);
+#pragma unroll
+  for (int k = T / 2; k >= 1; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
   const float ref = m == -INFINITY ? 0.0f : m;
-  float den = 0.0f;
-  for (int i = lane_id(); i < pieces; i += kWave) {
+  for (int i = t; i < pieces; i += T) {
     const float2 ml = p.part_ml[base + (int64_t)i * p.max_rows];
     den += ml.y * __builtin_amdgcn_exp2f(ml.x - ref);
   }
-  den = wave_sum(den);
-  float o = 0.0f;
-#pragma unroll 8
+#pragma unroll
+  for (int k = T / 2; k >= 1; k >>= 1) den += __shfl_xor(den, k);
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
   for (int i = g; i < pieces; i += G) {
     const int64_t at = base + (int64_t)i * p.max_rows;
-    o += p.part[at * D + d] * __builtin_amdgcn_exp2f(p.part_ml[at].x - ref);
+    const float f = __builtin_amdgcn_exp2f(p.part_ml[at].x - ref);
+    const float4 x = reinterpret_cast<const float4*>(p.part + at * D)[t];
+    o.x += x.x * f;
+    o.y += x.y * f;
+    o.z += x.z * f;
+    o.w += x.w * f;
   }
-  red[g][d] = o;
+  red[s][t] = o;
   __syncthreads();
-  if (g == 0) {
-#pragma unroll
-    for (int i = 1; i < G; ++i) o += red[i][d];
-    p.out[(int64_t)(tl.q0 + r / p.group) * p.ldo + (int64_t)(j * p.group + r % p.group) * D + d] =
-        float_to_bf16_bits(den == 0.0f ? 0.0f : o / den);
+  if (g != 0 || r >= rows) return;
+  for (int i = 1; i < G; ++i) {
+    const float4 x = red[s + i][t];
+    o.x += x.x;
+    o.y += x.y;
+    o.z += x.z;
+    o.w += x.w;
   }
+  auto bits = [&](float x) { return (uint32_t)float_to_bf16_bits(den == 0.0f ? 0.0f : x / den); };
+  uint16_t* dst = p.out + (int64_t)(work.t.q0 + r / p.group) * p.ldo + (int64_t)(j * p.group + r % p.group) * D + 4 * t;
+  *reinterpret_cast<uint2*>(dst) = make_uint2(bits(o.x) | (bits(o.y) << 16), bits(o.z) | (bits(o.w) << 16));
 }
 
 // ------------------------------------------------------------------ more than 16 rows
@@ -856,29 +945,27 @@ __global__ __launch_bounds__(256) void attn_tile_join_kernel(PagedAttnParams p) 
 
 // ------------------------------------------------------------------ launches
 
-// Row kernel: as many pieces as give about four workgroups a CU if every context is
-// as long as it may be, of whole passes of the workgroup's waves (128 keys).
-static constexpr int kPieceTarget = 1024;
+// Row kernel: workgroups that the CUs hold at once, two each.
+static constexpr int64_t kRowSlots = 512;
 // Tile kernel: pieces for one workgroup a CU at least, of 512 keys and more: a
 // piece writes its 128 rows in binary32 and they are read again to be joined.
-static constexpr int kTileTarget = 512, kTilePieceMin = 512;
+static constexpr int kTileTarget = 384, kTilePieceMin = 512;
 
 void attn_paged_plan(PagedAttnParams* p, int64_t max_q, int64_t ctx_max) {
   const int64_t span = std::min<int64_t>(ctx_max, (int64_t)p->window + max_q) + kStep;  // keys of any row and its neighbours
   p->max_q = (int)max_q;
   p->max_rows = (int)std::min<int64_t>(max_q * p->group, kRows);
-  int64_t most = std::max<int64_t>(kPieceTarget / ((int64_t)p->batch.n_seqs * p->kv.n_kv), 1);
-  int64_t piece = (span + most - 1) / most;
-  piece = (piece + kPass - 1) / kPass * kPass;
-  p->piece = (int)piece;
-  p->max_pieces = (int)((span + piece - 1) / piece);
+  // pieces for each key/value head: the slots, or of more sequences than slots two rounds
+  // of them; more than that fill the CUs whole
+  const int64_t rounds = (p->batch.n_seqs * (int64_t)p->kv.n_kv + kRowSlots - 1) / kRowSlots;
+  p->row_pieces = p->batch.n_seqs <= kSplitSeqs && rounds <= 2 && span > kPass ? (int)(kRowSlots * rounds / p->kv.n_kv) : 0;
   p->tile_slots = 0;
   p->tile_piece = p->max_tile_pieces = 1;
   if (max_q * p->group > kRows) {
     p->tile_slots = (int)(p->rows * p->group / kTile + p->batch.n_seqs);
     const int64_t tiles = (p->rows * p->group / kTile + 1) * p->kv.n_kv;
-    most = (kTileTarget + tiles - 1) / tiles;
-    piece = std::max<int64_t>((span + most - 1) / most, kTilePieceMin);
+    const int64_t most = (kTileTarget + tiles - 1) / tiles;
+    int64_t piece = std::max<int64_t>((span + most - 1) / most, kTilePieceMin);
     piece = (piece + 2 * kStep - 1) / (2 * kStep) * (2 * kStep);
     p->tile_piece = (int)piece;
     p->max_tile_pieces = (int)((span + piece - 1) / piece);
@@ -888,7 +975,7 @@ void attn_paged_plan(PagedAttnParams* p, int64_t max_q, int64_t ctx_max) {
 // Workspace: outputs of the row kernel's pieces, of the tile kernel's, then their
 // maxima and sums.
 static size_t row_parts(const PagedAttnParams& p) {
-  return p.max_pieces == 1 ? 0 : (size_t)p.batch.n_seqs * p.kv.n_kv * p.max_pieces * p.max_rows;
+  return (size_t)p.kv.n_kv * p.row_pieces * p.max_rows;
 }
 static size_t tile_parts(const PagedAttnParams& p) {
   return p.max_tile_pieces == 1 ? 0 : (size_t)p.tile_slots * p.kv.n_kv * p.max_tile_pieces * kTile;
@@ -929,10 +1016,10 @@ static hipError_t paged_launch(PagedAttnParams p, void* ws, hipStream_t st) {
     const hipError_t e = tile_launch<D, I8>(p, st);
     if (e != hipSuccess) return e;
   }
-  attn_rows_kernel<D, I8><<<dim3((unsigned)p.batch.n_seqs, (unsigned)p.kv.n_kv, (unsigned)p.max_pieces), 256, 0, st>>>(p);
+  attn_rows_kernel<D, I8><<<dim3((unsigned)(p.row_pieces ? p.row_pieces : p.batch.n_seqs), (unsigned)p.kv.n_kv), 256, 0, st>>>(p);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.max_pieces == 1) return e;
-  attn_join_kernel<D><<<dim3((unsigned)p.batch.n_seqs, (unsigned)p.kv.n_kv, (unsigned)p.max_rows), 1024, 0, st>>>(p);
+  if (e != hipSuccess || !p.row_pieces) return e;
+  attn_join_kernel<D><<<dim3((unsigned)p.batch.n_seqs, (unsigned)p.kv.n_kv), 1024, 0, st>>>(p);
   return hipGetLastError();
 }
 

@@ -69,6 +69,31 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v + lane_xor<1>(v);
 }
 
+// Inclusive scan over a wave: shifts within rows of 16 lanes, then each row's last
+// lane to the rows after it, without an LDS round trip a step (a chain of 18 of
+// them, in the scans of sample_draw_kernel, took 4 of its 25 us).  Lanes that get
+// nothing add 0.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = moved<CTRL, ROWS>((uint32_t)b), hi = moved<CTRL, ROWS>((uint32_t)(b >> 32));
+  return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+template <class T>
+__device__ __forceinline__ T wave_scan(T v) {
+  v += moved<0x111, 0xF>(v);  // from the lane 1 before, 2, 4, 8
+  v += moved<0x112, 0xF>(v);
+  v += moved<0x114, 0xF>(v);
+  v += moved<0x118, 0xF>(v);
+  v += moved<0x142, 0xA>(v);  // lane 15 of rows 0 and 2 to rows 1 and 3
+  v += moved<0x143, 0xC>(v);  // lane 31 to rows 2 and 3
+  return v;
+}
+
 __device__ __forceinline__ int lane_id() { return (int)(threadIdx.x & (kWave - 1)); }
 
 // Byte offset of fragment (rb, kb) in a packed matrix with kb_count fragment columns.

@@ -361,9 +361,10 @@ struct PagedAttnParams {
   float scale_log2 = 0.0f;        // score scale times log2(e)
   PagedKv kv;
   PagedBatch batch;
-  // set by attn_paged_plan: keys of a piece of the row kernel's work, most pieces
-  // and rows of a sequence; tiles of the tile kernel (0: not needed), the same of it
-  int max_q = 0, piece = 0, max_pieces = 0, max_rows = 0;
+  // set by attn_paged_plan: pieces of the row kernel's work for each key/value head
+  // (0: its sequences whole) and most rows of a sequence; tiles of the tile kernel
+  // (0: not needed), keys of a piece of theirs and most of them
+  int max_q = 0, row_pieces = 0, max_rows = 0;
   int tile_slots = 0, tile_piece = 0, max_tile_pieces = 0;
   // set by the launcher: partial results
   float* part = nullptr;

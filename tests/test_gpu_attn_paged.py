@@ -182,3 +182,53 @@ def test_one_token_agrees_with_the_contiguous_cache(int8):
         # both within half a step of nearly the same binary32 result: at most one step apart
         a, c = out.view(-1).double(), want.double()
         assert ((a - c).abs() <= 2.0 ** -7 * c.abs() + 2.0 ** -16 * c.abs().max()).all()
+
+
+@pytest.mark.parametrize("seqs,n_kv", [(70, 1), (130, 2), (200, 4), (300, 4), (513, 1), (520, 3)])
+def test_contexts_of_many_lengths(seqs, n_kv):
+    """A few long contexts among many short ones: sequences in one piece and in
+    several, more of them than workgroups fit, and more than are shared out."""
+    fresh = [(0 if i % 13 == 5 else 1 + i % 2) for i in range(seqs)]
+    ctx = [f + (5 * i) % 60 + (2500 if i in (3, seqs - 2) else 0) for i, f in enumerate(fresh)]
+    attend(Paged(fresh, ctx, n_kv, 128, 64, True, seed=seqs), n_kv)
+
+
+@pytest.mark.parametrize("int8", [True, False])
+@pytest.mark.parametrize("d", [128, 256])
+@pytest.mark.parametrize("window,holes", [(None, ()), (700, ()), (None, range(20, 60)), (300, range(40, 131))])
+def test_tiles_in_pieces(d, int8, window, holes):
+    """More than 16 rows over keys that several workgroups share, with a window and
+    with pages given back."""
+    h = Paged([45, 2], [2100, 1300], 2, d, 16, int8, seed=d, holes={(0, i) for i in holes})
+    attend(h, 6, window)
+
+
+@pytest.mark.parametrize("int8", [True, False])
+def test_more_new_tokens_than_announced(int8):
+    """A sequence of more new tokens than max_q is left alone; the others are not."""
+    h = Paged([3, 40, 2], [50, 60, 70], 1, 128, 16, int8, seed=8)
+    q = torch.randn((45, 2, 128), generator=serving.gen(9)).to(torch.bfloat16).to(DEV)
+    good = w8a8.attn_paged(q, h.cache(w8a8), h.batch(w8a8))
+    b = h.batch(w8a8)
+    for max_q in (39, 3):
+        b.max_q = max_q
+        out = torch.full_like(q, 2.0)
+        w8a8.attn_paged(q, h.cache(w8a8), b, out=out)
+        assert (out[3:43] == 2.0).all()
+        for s in (slice(0, 3), slice(43, 45)):  # cut into other pieces, perhaps
+            assert (out[s].float() - good[s].float()).abs().max() <= 2.0 ** -7 * good.float().abs().max()
+
+
+def test_workspace():
+    h = Paged([1, 30], [600, 700], 1, 256, 64, True, seed=3)
+    q = torch.randn((31, 4, 256), generator=serving.gen(3)).to(torch.bfloat16).to(DEV)
+    cache, b = h.cache(w8a8), h.batch(w8a8)
+    need = w8a8.attn_paged_workspace_bytes(31, 4, 1, 256, 2, b.max_q, b.table.shape[1] * 64)
+    assert need > 0
+    good = w8a8.attn_paged(q, cache, b)
+    ws = torch.full((need + 256,), 0x7f, dtype=torch.uint8, device=DEV)
+    assert torch.equal(w8a8.attn_paged(q, cache, b, ws=ws[:need]), good)
+    assert (ws[need:] == 0x7f).all()
+    with pytest.raises(w8a8.W8A8Error) as e:
+        w8a8.attn_paged(q, cache, b, ws=ws[:need - 256])
+    assert e.value.status == w8a8.EWORKSPACE
