@@ -472,24 +472,34 @@ typedef short v4s __attribute__((ext_vector_type(4)));
 __device__ v4i kZeros = {0, 0, 0, 0};  // what stands for a row that is not read
 typedef const __attribute__((address_space(1))) v4i* GlobalVec;
 
-// A tile of a sequence of more than 16 rows.  Sequence s has the slots floor(q_start[s] *
-// group / kTile) + s and up, one for each of its tiles at least: a workgroup finds
-// its sequence without a prefix sum, and the slots left between are empty.
-__device__ __forceinline__ bool tile_of(const PagedAttnParams& p, int64_t slot, Seq* t, int* seq, int* row0) {
-  int count = 0;
+// Tiles of sequence s, of the sequences of more than 16 rows.
+__device__ __forceinline__ uint32_t tiles_of(const PagedAttnParams& p, int s) {
+  Seq t;
+  if (s >= p.batch.n_seqs || !seq_at(p, p.batch.q_start[s], p.batch.q_start[s + 1], 0, &t)) return 0;
+  const int rows = t.q_len * p.group;
+  return rows > kRows ? (uint32_t)((rows + kTile - 1) / kTile) : 0u;
+}
+// all tiles of the batch
+__device__ __forceinline__ int count_tiles(const PagedAttnParams& p) {
+  uint32_t n = 0;
+  for (int base = 0; base < p.batch.n_seqs; base += kWave) n += tiles_of(p, base + lane_id());
+  return (int)min(total(n), (uint32_t)p.tile_slots);  // fewer than counted only where sequences overlap
+}
+// tile number `tile`, sequence by sequence; false: none
+__device__ __forceinline__ bool tile_of(const PagedAttnParams& p, int tile, Seq* t, int* seq, int* row0) {
+  uint32_t before = 0;
   for (int base = 0; base < p.batch.n_seqs; base += kWave) {
-    const int s = base + lane_id();
-    const uint64_t m = __ballot(s < p.batch.n_seqs && (int64_t)p.batch.q_start[min(s, p.batch.n_seqs)] * p.group / kTile + s <= slot);
-    count += __popcll(m);
-    if (m != ~0ull) break;
+    const uint32_t mine = tiles_of(p, base + lane_id()), upto = before + wave_scan(mine);
+    const uint64_t hit = __ballot(upto - mine <= (uint32_t)tile && (uint32_t)tile < upto);
+    if (hit) {
+      const int at = __builtin_ctzll(hit);
+      *seq = base + at;
+      *row0 = (tile - __builtin_amdgcn_readlane((int)(upto - mine), at)) * kTile;
+      return seq_of(p, base + at, t);
+    }
+    before = (uint32_t)__builtin_amdgcn_readlane((int)upto, kWave - 1);
   }
-  if (count == 0) return false;
-  count = __builtin_amdgcn_readfirstlane(count);
-  *seq = count - 1;
-  if (!seq_of(p, count - 1, t)) return false;
-  const int64_t r = (slot - (int64_t)t->q0 * p.group / kTile - (count - 1)) * kTile, rows = (int64_t)t->q_len * p.group;
-  *row0 = (int)r;
-  return r >= 0 && r < rows && rows > kRows;
+  return false;
 }
 
 __device__ __forceinline__ v16f mma32_bf16(v4i a, v4i b, v16f c) {
@@ -566,8 +576,14 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
 
   Seq tl;
   int seq, row0;
-  const int64_t slot = (int64_t)gridDim.x - 1 - blockIdx.x;  // the longest ranges of keys first
-  const int j = blockIdx.y, split = blockIdx.z;
+  // The workgroups with work come first, without gaps: what is one round of the CUs is
+  // spread evenly over them.  With empty ones between, some of 256 equal pieces waited for
+  // another's end (64 tiles over 8192 keys: 126 us instead of 76).
+  const int n_tiles = count_tiles(p);
+  const uint32_t id = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z);
+  if (n_tiles == 0 || id >= (uint32_t)n_tiles * gridDim.y * gridDim.z) return;
+  const int slot = n_tiles - 1 - (int)(id % n_tiles);  // the longest ranges of keys first
+  const int j = (int)(id / n_tiles % gridDim.y), split = (int)(id / n_tiles / gridDim.y);
   if (!tile_of(p, slot, &tl, &seq, &row0)) return;  // whole workgroup
   const int rows = tl.q_len * p.group;
   const Keys ks = keys_of(p, tl, row0, min(row0 + kTile, rows) - 1, p.tile_piece);
@@ -905,7 +921,7 @@ __global__ __launch_bounds__(256) void attn_tile_join_kernel(PagedAttnParams p) 
   constexpr int NB = D / 32, Q = NB;  // float4 of a lane (NB * 4 / 4 waves)
   Seq tl;
   int seq, row0;
-  const int64_t slot = blockIdx.x;
+  const int slot = blockIdx.x;
   const int j = blockIdx.y, rg = blockIdx.z, w = threadIdx.x >> 6, l = lane_id(), n = l & 31, g = l >> 5;
   if (!tile_of(p, slot, &tl, &seq, &row0)) return;  // whole workgroup
   const int rows = tl.q_len * p.group, row = row0 + 32 * rg + n;
@@ -947,9 +963,12 @@ __global__ __launch_bounds__(256) void attn_tile_join_kernel(PagedAttnParams p) 
 
 // Row kernel: workgroups that the CUs hold at once, two each.
 static constexpr int64_t kRowSlots = 512;
-// Tile kernel: pieces for one workgroup a CU at least, of 512 keys and more: a
-// piece writes its 128 rows in binary32 and they are read again to be joined.
-static constexpr int kTileTarget = 384, kTilePieceMin = 512;
+// Tile kernel: pieces for one workgroup a CU, which is what one holds; for two where the
+// new tokens may be most of the context, as the keys of a prompt's tiles then differ from
+// few to all (one tile of a piece each: 200 us of the prompt of 8192 tokens instead of
+// 160).  Of 512 keys and more: a piece writes its 128 rows in binary32 and they are read
+// again to be joined.
+static constexpr int kTileSlots = 256, kTilePieceMin = 512;
 
 void attn_paged_plan(PagedAttnParams* p, int64_t max_q, int64_t ctx_max) {
   const int64_t span = std::min<int64_t>(ctx_max, (int64_t)p->window + max_q) + kStep;  // keys of any row and its neighbours
@@ -964,7 +983,7 @@ void attn_paged_plan(PagedAttnParams* p, int64_t max_q, int64_t ctx_max) {
   if (max_q * p->group > kRows) {
     p->tile_slots = (int)(p->rows * p->group / kTile + p->batch.n_seqs);
     const int64_t tiles = (p->rows * p->group / kTile + 1) * p->kv.n_kv;
-    const int64_t most = (kTileTarget + tiles - 1) / tiles;
+    const int64_t target = 2 * max_q > ctx_max ? 2 * kTileSlots : kTileSlots, most = (target + tiles - 1) / tiles;
     int64_t piece = std::max<int64_t>((span + most - 1) / most, kTilePieceMin);
     piece = (piece + 2 * kStep - 1) / (2 * kStep) * (2 * kStep);
     p->tile_piece = (int)piece;
