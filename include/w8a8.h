@@ -610,7 +610,10 @@ w8a8_status w8a8_kv_read(const w8a8_paged_kv* kv, const w8a8_paged_batch* batch,
    ldq and ldo (multiples of 8).  n_heads: a multiple of n_kv.  window >= 1
    (2^30 and more: none), scale finite (1 / sqrt(head_dim) as a rule).  Sums
    and softmax statistics are binary32.  Cached rows past ctx_len, before every
-   new token's window and in pages that are not held are never used.
+   new token's window and in pages that are not held are never used; a non-finite
+   value in a row that one of a sequence's new tokens attends may reach its other new
+   tokens.  The same call gives the same bits; how a context is cut into pieces, and
+   so the order of its sums, follows from the lengths of all sequences.
    ws: w8a8_attn_paged_workspace_bytes(...) bytes of the same sizes, with ctx_max =
    max_pages * page, the positions that the tables can hold (may be NULL when
    that is 0).  Calls that share a workspace must not overlap in time. */

@@ -159,6 +159,12 @@ __device__ __forceinline__ bool row_work(const PagedAttnParams& p, int slot, int
 // values are loaded as soon as the registers of this one's are free.  Rows of a
 // held page are read whatever they hold; what no row attends is masked out of the
 // scores, and zeroed in bf16 values (a weight of 0 times NaN).
+//
+// Memory bounds it: 64 contexts of 2048 to 16384 positions (240 MB of INT8) take 52 us,
+// 4.6 TB/s with the 6 us before the first loads return and the last workgroups' ends
+// (without the conversions or half the products 3 to 8 us less); 40 windows of 1024
+// (131 MB of bf16) 32 us.  Registers for two workgroups a CU: with one, the windows took
+// 5 us more.
 template <int D, bool I8>
 __global__ __launch_bounds__(256, 2) void attn_rows_kernel(PagedAttnParams p) {
   constexpr int KI = I8 ? D / 64 : D / 32;  // 16-byte pieces of a lane's quarter of a key row
@@ -412,7 +418,8 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(PagedAttnParams p) {
 
 // The pieces of a sequence's rows, one workgroup for all of them: D / 4 threads have four
 // dimensions of a row each, and where there are few rows several such groups add
-// every G-th piece; the groups' sums are added in order.
+// every G-th piece; the groups' sums are added in order.  6 to 7 us, of which the launch
+// and finding the pieces are 5; a workgroup for each row took 15 of 40 x 4 sequences' heads.
 template <int D>
 __global__ __launch_bounds__(1024) void attn_join_kernel(PagedAttnParams p) {
   constexpr int T = D / 4, S = 1024 / T;
@@ -559,11 +566,19 @@ __device__ __forceinline__ void load_lds16_rows(const char* from, uint32_t off, 
 // what is read in one cycle (the same chunk of 16 key rows; 64 bytes of four value
 // rows) covers the 64 banks once.  INT8 codes become
 // bf16 (exactly) on the way into LDS, once for the four row groups; a key's scale
-// multiplies its scores, a value's its weight.  The weights are rounded to bf16: 2^-9
-// on average of each, independent of each other, below the result's own rounding.
+// multiplies its scores, a value's its weight.  The weights are rounded to bf16, each
+// by half a step (2^-8 of it) at most and independently of the others, which moves a
+// result by less than its own rounding to bf16 where several keys share the weight.
 // The reference of the exponentials follows the running maximum only when that
 // has grown by 2^8, so that the outputs are seldom rescaled (binary32 sums have the
 // room, and the rounding of the weights is relative).
+//
+// 8192 tokens of one prompt, 4 heads of 256, bf16: 160 us, 0.86 PFLOP/s of the pairs
+// that are attended, where a large library product reaches 1.27.  A step of 64 keys takes
+// 7000 cycles of a SIMD: 2 x 1024 of matrix instructions, and between them the reads of
+// LDS, 100 vector instructions and 16 exponentials of 4 cycles and more a wave, and two
+// barriers.  509 tokens over 8192 positions, 16 heads of 128, INT8: 75 us; vector
+// instructions bound it (codes to bf16, two scales, weights).
 template <int D, bool I8>
 __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
   constexpr int NC = D / 16, NB = D / 32;  // 16-dimension steps of a score, 32-dimension blocks of a result
@@ -915,7 +930,8 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
 }
 
 // The pieces of a tile: a workgroup joins 32 rows, each of its waves a quarter of
-// their dimensions, in the layout the pieces are in.
+// their dimensions, in the layout the pieces are in (11.6 us for the 43 MB of the prompt
+// of 8192 tokens, whose pieces the memory-side cache holds).
 template <int D>
 __global__ __launch_bounds__(256) void attn_tile_join_kernel(PagedAttnParams p) {
   constexpr int NB = D / 32, Q = NB;  // float4 of a lane (NB * 4 / 4 waves)
@@ -981,7 +997,8 @@ void attn_paged_plan(PagedAttnParams* p, int64_t max_q, int64_t ctx_max) {
   p->tile_slots = 0;
   p->tile_piece = p->max_tile_pieces = 1;
   if (max_q * p->group > kRows) {
-    p->tile_slots = (int)(p->rows * p->group / kTile + p->batch.n_seqs);
+    // a last tile for each sequence of more than kRows rows
+    p->tile_slots = (int)(p->rows * p->group / kTile + std::min<int64_t>(p->batch.n_seqs, p->rows * p->group / (kRows + 1)));
     const int64_t tiles = (p->rows * p->group / kTile + 1) * p->kv.n_kv;
     const int64_t target = 2 * max_q > ctx_max ? 2 * kTileSlots : kTileSlots, most = (target + tiles - 1) / tiles;
     int64_t piece = std::max<int64_t>((span + most - 1) / most, kTilePieceMin);
