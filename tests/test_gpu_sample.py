@@ -200,3 +200,19 @@ def test_workspace_refusal():
     with pytest.raises(w8a8.W8A8Error) as e:
         w8a8.sample(l, u, ws=torch.empty(need - 1, dtype=torch.uint8, device=DEV))
     assert e.value.status == w8a8.EWORKSPACE
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("centre", [0.5, -0.5, 0.0])
+@pytest.mark.parametrize("n", [70, 300, 1001, 3001, 9001, 20001])
+def test_many_values_close_together(n, centre, dt):
+    """Logits within 0.02 of each other, up to thousands of different ones in a bin,
+    at odd row starts (-0 among them): every filter ends among them."""
+    g = serving.gen(n)
+    l = (centre + 0.02 * (torch.rand((4, n), generator=g) - 0.5)).to(dt)
+    l[:, ::50] *= -0.0 if centre == 0.0 else 1.0
+    u = uniform(4, n)
+    check(l, u, k=torch.tensor([1, n // 7, n // 2, n - 1], dtype=torch.int32), ld=n + 3)
+    check(l, u, p=torch.tensor([0.001, 0.3, 0.6, 0.995]))
+    check(l, u, m=torch.tensor([0.999, 0.993, 0.985, 0.981]))
+    check(l, u, t=0.01, k=n // 2, p=0.7, m=0.3)

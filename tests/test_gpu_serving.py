@@ -156,3 +156,42 @@ def test_a_stream_of_its_own():
         s.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(got, want))
     assert torch.cuda.current_stream() != s
+
+
+@pytest.mark.parametrize("int8", [True, False])
+def test_prompts_captured_and_replayed(int8):
+    """Append and attention captured for up to 96 rows of four sequences, replayed
+    with other lengths: prompts beside single tokens, single tokens only, one long
+    sequence, none at all; against the eager calls, rows behind the last sequence untouched."""
+    m, rows = Model(), 96
+    g = serving.gen(11)
+    caches = [w8a8.PagedKV.empty(4 * 70, 16, int8=int8) for _ in range(2)]
+    table = torch.randperm(4 * 70, generator=g).int().view(4, 70).to(DEV)
+    b = w8a8.PagedBatch(table, torch.zeros(5, dtype=torch.int32, device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV), 90)
+    qkv = torch.zeros((rows, (HEADS + 2) * 256), dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(w8a8.attn_paged_workspace_bytes(rows, HEADS, 1, 256, 4, 90, 70 * 16), dtype=torch.uint8, device=DEV)
+    q, out = (torch.zeros((rows, HEADS, 256), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+
+    def step(cache, q, out):
+        w8a8.kv_append(qkv, cache, b, HEADS, rope=m.rope, out=q)
+        w8a8.attn_paged(q, cache, b, out=out, ws=ws)
+
+    gr = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr):
+        step(caches[0], q, out)
+    done = [0, 0, 0, 0]
+    for fresh in ([40, 1, 0, 20], [1, 1, 1, 1], [0, 90, 0, 0], [0, 0, 0, 0], [17, 16, 33, 30], [1, 0, 70, 2]):
+        done = [d + f for d, f in zip(done, fresh)]
+        qkv.copy_(torch.randn(qkv.shape, generator=g))
+        b.q_start.copy_(torch.tensor([0] + fresh).cumsum(0))
+        b.ctx_len.copy_(torch.tensor(done))
+        q.fill_(3.0)
+        out.fill_(3.0)
+        want_q, want = torch.full_like(q, 3.0), torch.full_like(out, 3.0)
+        step(caches[1], want_q, want)
+        torch.cuda.synchronize()
+        gr.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(q, want_q) and torch.equal(out, want), fresh
+        assert (out[sum(fresh):] == 3.0).all()
+        assert torch.equal(caches[0].k, caches[1].k) and torch.equal(caches[0].v, caches[1].v)
