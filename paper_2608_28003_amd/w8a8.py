@@ -1058,12 +1058,15 @@ def sample_workspace_bytes(rows, n, dtype):
 
 def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, prob=None, ws=None, stream=None):
     """One token for each row of logits (bf16 or f32 [rows, n], unit column
-    stride) from the uniform numbers u (float32 [rows]): (tokens int64, the
-    probability each was drawn with).  temperature, top_p, min_p: a number or
+    stride, rows that do not overlap) from the uniform numbers u (float32 [rows]):
+    (tokens int64, the probability each was drawn with).  temperature, top_p, min_p: a number or
     float32 [rows]; top_k: a number or int32 [rows]; None: off."""
     if not logits.is_cuda or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits must be a GPU tensor [rows, n] with unit column stride")
     rows, n = logits.shape
+    ld = logits.stride(0) if rows > 1 else n
+    if ld < n:  # expanded rows, or windows over a vector
+        raise ValueError("logits must have rows that do not overlap")
     device, dt = logits.device, _dt(logits)
     _need(u, "u", torch.float32, device, (rows,))
     d = SampleDesc(None, 1.0, None, 0, None, 1.0, None, 0.0)
@@ -1082,9 +1085,8 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, 
             ws = _empty(lib().w8a8_sample_workspace_bytes(rows, n, dt), device)
         elif ws.device != device:
             raise ValueError("ws must be on the logits' device")
-        _check(lib().w8a8_sample(ctypes.byref(d), logits.data_ptr(), dt, rows, n,
-                                 max(n, logits.stride(0) if rows > 1 else n), u.data_ptr(), out.data_ptr(),
-                                 prob.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), st))
+        _check(lib().w8a8_sample(ctypes.byref(d), logits.data_ptr(), dt, rows, n, ld, u.data_ptr(),
+                                 out.data_ptr(), prob.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), st))
     return out, prob
 
 
