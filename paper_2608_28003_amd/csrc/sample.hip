@@ -1067,7 +1067,7 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p, C
     uint32_t todo = 0;  // logits that need an exponential: few of a bf16 row's, so one a lane at a time
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
-      const int b = first - place_of(k[e]);
+      const int b = min(first - place_of(k[e]), kBins - 1);  // the last one: all below the bins
       x[e] = 0.0;
       if (k[e] && b <= bin && (b < kBins - 1 || bin == kBins)) {
         if (b == bin && single) {
