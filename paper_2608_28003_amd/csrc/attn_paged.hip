@@ -75,6 +75,13 @@ __device__ __forceinline__ Keys keys_of(const PagedAttnParams& p, const Seq& t, 
   k.pieces = max((k.hi - k.begin + piece - 1) / piece, 1);
   return k;
 }
+// Where the piece of `piece` keys from `begin` on ends, of keys up to hi.  (The sum of
+// begin and piece can pass 32 bits: a context beyond a table of 2^30 positions.)
+__host__ __device__ constexpr int piece_end(int begin, int hi, int piece) {
+  return hi - begin < piece ? hi : begin + piece;
+}
+static_assert(piece_end((1 << 30) - 32, 1 << 30, 1 << 30) == 1 << 30, "the last keys of the largest table");
+static_assert(piece_end(0, -(1 << 30), 512) == -(1 << 30) && piece_end(512, 2000, 512) == 1024, "no keys; a piece in the middle");
 
 // Work of the row kernel: a sequence of at most 16 rows, or a piece of its keys.
 //
@@ -182,7 +189,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(PagedAttnParams p) {
   const Keys ks = work.ks;
   const int seq = work.seq, rows = tl.q_len * p.group, split = slot - work.slot0;
   if (split >= ks.pieces) return;
-  const int begin = ks.begin + split * work.piece, lo = ks.lo, hi = min(ks.hi, begin + min(work.piece, ks.hi - begin));
+  const int begin = ks.begin + split * work.piece, lo = ks.lo, hi = piece_end(begin, ks.hi, work.piece);
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = lane_id(), n = l & 15, g = l >> 4;
   const int pos = n < rows ? tl.first + n / p.group : -1;
   const int from = pos < 0 ? 0 : max(0, pos + 1 - p.window);
@@ -603,7 +610,7 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
   const int rows = tl.q_len * p.group;
   const Keys ks = keys_of(p, tl, row0, min(row0 + kTile, rows) - 1, p.tile_piece);
   if (split >= ks.pieces) return;
-  const int begin = ks.begin + split * p.tile_piece, lo = ks.lo, hi = min(ks.hi, begin + p.tile_piece);
+  const int begin = ks.begin + split * p.tile_piece, lo = ks.lo, hi = piece_end(begin, ks.hi, p.tile_piece);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane_id(), n = l & 31, g = l >> 5;
   const int rg = w & 3, kg = w >> 2;
   const int wrow = row0 + 32 * rg, row = wrow + n;       // the wave's first row, the lane's row
@@ -997,7 +1004,8 @@ static constexpr int64_t kRowSlots = 512;
 static constexpr int kTileSlots = 256, kTilePieceMin = 512;
 
 void attn_paged_plan(PagedAttnParams* p, int64_t max_q, int64_t ctx_max) {
-  const int64_t span = std::min<int64_t>(ctx_max, (int64_t)p->window + max_q) + kStep;  // keys of any row and its neighbours
+  // keys of any row and its neighbours; no key lies behind the 2^30 positions of the largest table
+  const int64_t span = std::min<int64_t>(std::min<int64_t>(ctx_max, (int64_t)p->window + max_q) + kStep, 1 << 30);
   p->max_q = (int)max_q;
   p->max_rows = (int)std::min<int64_t>(max_q * p->group, kRows);
   // pieces for each key/value head: the slots, or of more sequences than slots two rounds
