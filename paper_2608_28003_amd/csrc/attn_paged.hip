@@ -83,6 +83,13 @@ __host__ __device__ constexpr int piece_end(int begin, int hi, int piece) {
 static_assert(piece_end((1 << 30) - 32, 1 << 30, 1 << 30) == 1 << 30, "the last keys of the largest table");
 static_assert(piece_end(0, -(1 << 30), 512) == -(1 << 30) && piece_end(512, 2000, 512) == 1024, "no keys; a piece in the middle");
 
+// The sum of all passes over the slots, rounded up: the fewest passes of a piece.  The sum
+// is one modulo 2^32: of 512 sequences of 2^30 positions, 2^32 passes, it is 0, which
+// means nothing else (without any pass no answer is used).
+__host__ __device__ constexpr uint32_t fewest_passes(uint32_t sum, uint32_t slots) { return (sum - 1) / slots + 1; }
+static_assert(fewest_passes(0, kSplitSeqs) == 1u << 23, "512 sequences of 2^30 positions");
+static_assert(fewest_passes(1, 512) == 1 && fewest_passes(512, 512) == 1 && fewest_passes(513, 512) == 2, "rounded up");
+
 // Work of the row kernel: a sequence of at most 16 rows, or a piece of its keys.
 //
 // Contexts differ by much and only the GPU knows them, so the pieces are counted here:
@@ -113,9 +120,8 @@ __device__ __forceinline__ bool row_work(const PagedAttnParams& p, int slot, int
       }
       sum += k[c];
     }
-    sum = total(sum);
     const uint32_t slots = (uint32_t)p.row_pieces;
-    len = max((sum + slots - 1) / slots, 1u);
+    len = max(fewest_passes(total(sum), slots), 1u);
     for (;;) {  // to the longest at the latest: a piece a sequence, of which there are no more than slots
       uint32_t n = 0;
 #pragma unroll
