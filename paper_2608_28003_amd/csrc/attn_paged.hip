@@ -549,7 +549,7 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {  // one v_cvt_pk
 // tile; the wait is at the barrier that ends the buffer's filling.
 __device__ __forceinline__ void load_lds16(GlobalVec src, uint32_t lds) {
   lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(lds) : "memory");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(lds) : "m0", "memory");
 }
 // N such loads 1024 bytes apart, both in LDS and from `from` (wave-uniform); load i at
 // lane offset off ^ (s1 if i is odd) ^ (s2 if i >= 2).
@@ -562,10 +562,10 @@ __device__ __forceinline__ void load_lds16_rows(const char* from, uint32_t off, 
   if constexpr (N == 4)
     asm volatile("s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024\n\t"
                  "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072"
-                 : : "v"(off), "v"(off ^ s1), "v"(off ^ s2), "v"(off ^ s1 ^ s2), "s"(base), "s"(lds) : "memory");
+                 : : "v"(off), "v"(off ^ s1), "v"(off ^ s2), "v"(off ^ s1 ^ s2), "s"(base), "s"(lds) : "m0", "memory");
   else
     asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024"
-                 : : "v"(off), "v"(off ^ s1), "s"(base), "s"(lds) : "memory");
+                 : : "v"(off), "v"(off ^ s1), "s"(base), "s"(lds) : "m0", "memory");
 }
 // 128 rows of a sequence.  Eight waves, four row groups of 32 rows times two key
 // groups: key group k takes the 32-key tiles k, k + 2, ... of the piece, from its
