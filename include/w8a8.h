@@ -644,7 +644,11 @@ typedef struct {
    top_p of theirs; of these the tokens with w_i >= min_p.  One token always
    stays.  The token drawn is the first index i (in index order) with
    sum_{kept j <= i} w_j > u sum_{kept} w_j; u below 0 or NaN draws the first
-   kept token, 1 and more the last.  Weights and sums are binary64.  Logits of -inf and NaN
+   kept token, 1 and more the last.  Weights are binary64; so are sums, but those of many
+   logits, which are 64-bit integers, the same in any order: in units of 2^-48 of the largest
+   weight among 16384 neighbours and, for the border of top_p, of 2^-(62 - ceil(log2 n)) of
+   the row's largest weight (2^-44 of 262144 logits), where what 16384 neighbours of nearly
+   equal value weigh together is rounded to whole units.  Logits of -inf and NaN
    are never drawn; of +inf ones each has weight 1 and all others 0.  A row with
    nothing to draw gives token -1 (and prob 0).
    u: DEVICE float[rows]; token: DEVICE int64[rows]; prob: DEVICE float[rows] or

@@ -216,16 +216,38 @@ __device__ int64_t walk(const Row& r, double u, bool share, F f, double* sums, d
   return found[0] != INT64_MAX ? found[0] : found[1];
 }
 
-// Digit by digit, the key of the logit at which the running measure over the
-// descending order reaches `goal`; *above: the measure of the larger keys.
+// Sums of weights that do not depend on the order: hi + lo / unit in units of 1 / unit, a
+// power of two with which all n weights of a row stay below 2^63, so that a weight counts
+// down to 1 / unit^2 (2^-76 of 2^24 logits, 2^-88 of 262144).
+struct Sum2 {
+  unsigned long long hi, lo;  // lo < unit
+};
+__device__ __forceinline__ void add2(Sum2& a, unsigned long long hi, unsigned long long lo, int bits) {
+  lo += a.lo;
+  a.hi += hi + (lo >> bits);
+  a.lo = lo & ((1ull << bits) - 1);
+}
+// x >= 0 as such a sum, its last part rounded by `round`
+template <class R>
+__device__ __forceinline__ void split2(double x, double unit, R round, unsigned long long* hi, unsigned long long* lo) {
+  const double h = floor(x * unit);
+  *hi = (unsigned long long)h;
+  *lo = (unsigned long long)round((x * unit - h) * unit);
+}
+
+// Digit by digit, the key of the logit at which the running sum of f(key) over the
+// descending order reaches `goal`; *above: the sum of the larger keys.  unit: 2^bits.
 template <class F>
-__device__ uint32_t select(const Row& r, double goal, F f, unsigned long long* hist, uint32_t* pick, double unit, double* above) {
+__device__ uint32_t select(const Row& r, double goal, F f, unsigned long long (*hist)[2], uint32_t* pick, int bits, double* above) {
   uint32_t prefix = 0;
-  unsigned long long over = 0;
-  const unsigned long long want = (unsigned long long)ceil(goal * unit);
+  const double unit = ldexp(1.0, bits);
+  Sum2 over = {0, 0}, want = {0, 0};
+  unsigned long long hi, lo;
+  split2(goal, unit, [](double x) { return ceil(x); }, &hi, &lo);
+  add2(want, hi, lo, bits);
   for (int shift = 24; shift >= 0; shift -= 8) {
     __syncthreads();
-    if (threadIdx.x < 256) hist[threadIdx.x] = 0;
+    if (threadIdx.x < 256) hist[threadIdx.x][0] = hist[threadIdx.x][1] = 0;
     __syncthreads();
     for (int64_t i = threadIdx.x * kVec; i < r.n; i += kBlock) {
       uint32_t ks[kVec];
@@ -233,31 +255,32 @@ __device__ uint32_t select(const Row& r, double goal, F f, unsigned long long* h
       for (int e = 0; e < kVec; ++e) {
         const uint32_t k = ks[e];
         if (i + e < r.n && (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8)))) {
-          const unsigned long long v = f(k);
-          if (v) atomicAdd(&hist[(k >> shift) & 255], v);
+          split2(f(k), unit, [](double x) { return rint(x); }, &hi, &lo);
+          if (hi) atomicAdd(&hist[(k >> shift) & 255][0], hi);
+          if (lo) atomicAdd(&hist[(k >> shift) & 255][1], lo);
         }
       }
     }
     __syncthreads();
     if (threadIdx.x == 0) {
-      unsigned long long run = over;
+      Sum2 run = over, at = over;
       int last = -1;
-      unsigned long long at = over;
       for (int b = 255; b >= 0; --b) {
-        if (!hist[b]) continue;
+        if (!(hist[b][0] | hist[b][1])) continue;
         last = b;
         at = run;
-        run += hist[b];
-        if (run >= want) break;
+        add2(run, hist[b][0], hist[b][1], bits);
+        if (run.hi > want.hi || (run.hi == want.hi && run.lo >= want.lo)) break;
       }
       pick[0] = (uint32_t)max(last, 0);
-      hist[256] = at;
+      hist[256][0] = at.hi;
+      hist[256][1] = at.lo;
     }
     __syncthreads();
     prefix |= pick[0] << shift;
-    over = hist[256];
+    over = {hist[256][0], hist[256][1]};
   }
-  *above = (double)over;
+  *above = ((double)over.hi + (double)over.lo / unit) / unit;
   return prefix;
 }
 
@@ -265,7 +288,7 @@ __device__ uint32_t select(const Row& r, double goal, F f, unsigned long long* h
 struct PassLds {
   double sums[kMaxBlocks];
   double red[kThreads / kWave];
-  unsigned long long hist[257];
+  unsigned long long hist[257][2];
   int64_t found[2];
   uint32_t pick[1], tops[kThreads / kWave];
 };
@@ -299,7 +322,7 @@ __device__ __forceinline__ Row row_of(const SampleParams& p, int64_t row, bool b
 }
 
 // A row in passes over it, by a workgroup of kThreads.
-__device__ void draw_in_passes(const SampleParams& p, int64_t row, Row r, const RowArgs& a, double unit, PassLds& s) {
+__device__ void draw_in_passes(const SampleParams& p, int64_t row, Row r, const RowArgs& a, int bits, PassLds& s) {
   uint32_t top = 0;
   for (int64_t i = threadIdx.x * kVec; i < r.n; i += kBlock) {
     uint32_t k[kVec];
@@ -327,7 +350,7 @@ __device__ void draw_in_passes(const SampleParams& p, int64_t row, Row r, const 
   double ties = a.greedy ? 1.0 : 0.0, total;
   if (a.k_on) {
     double above;
-    thr = select(r, (double)a.top_k, [](uint32_t) { return 1ull; }, s.hist, s.pick, 1.0, &above);
+    thr = select(r, (double)a.top_k, [](uint32_t) { return 1.0; }, s.hist, s.pick, 0, &above);
     ties = (double)a.top_k - above;
   }
   if (a.p_on) {
@@ -344,10 +367,9 @@ __device__ void draw_in_passes(const SampleParams& p, int64_t row, Row r, const 
     if (floor_ties > 0.0) z += floor_ties * weight_call(r, floor_key);
     const double goal = (double)fmaxf(a.top_p, 0.0f) * z;
     double above;
-    thr = select(r, goal, [&](uint32_t k) {
-      return k >= floor_key ? (unsigned long long)rint(weight_call(r, k) * unit) : 0ull; }, s.hist, s.pick, unit, &above);
+    thr = select(r, goal, [&](uint32_t k) { return k >= floor_key ? weight_call(r, k) : 0.0; }, s.hist, s.pick, bits, &above);
     const double w = weight_call(r, thr);
-    ties = w > 0.0 ? fmax(1.0, ceil((goal - above / unit) / w)) : (double)r.n;
+    ties = w > 0.0 ? fmax(1.0, ceil((goal - above) / w)) : (double)r.n;
     if (floor_ties > 0.0 && thr == floor_key) ties = fmin(ties, floor_ties);
   }
   if (ties > 0.0)
@@ -681,13 +703,14 @@ __device__ __attribute__((noinline)) void gather_bin(const Row& r, DrawLds& s, c
 }
 
 template <bool BF>
-__global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p, ChunkWs ws, double unit) {
+__global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p, ChunkWs ws, int bits) {
   constexpr int kFixed = BF ? 2 * kBand : kBins;
   static_assert(kBins == 2 * kThreads && kList == 2 * kThreads && kChunk == 16 * kThreads, "a thread has two bins");
   __shared__ DrawUnion lds;
   DrawLds& s = lds.d;
   const int64_t row = blockIdx.x;
   const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6, C = ws.chunks;
+  const double unit = ldexp(1.0, bits);
   constexpr int kWaves = kThreads / kWave;
   const uint32_t* tops = ws.top + row * C;
   const uint16_t* count = ws.count + row * C * kBins;
@@ -948,7 +971,7 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p, C
   }
   if (lost) {
     __syncthreads();
-    draw_in_passes(p, row, r, a, unit, lds.p);
+    draw_in_passes(p, row, r, a, bits, lds.p);
     return;
   }
 
@@ -1132,12 +1155,12 @@ template <bool BF>
 hipError_t sample_launch(const SampleParams& p, void* ws, hipStream_t st) {
   int log2n = 0;
   while (((int64_t)1 << log2n) < p.n) ++log2n;
-  const double unit = ldexp(1.0, 62 - log2n);
+  const int bits = 62 - log2n;  // n weights up to 1 in units of 2^-bits stay below 2^63
   const ChunkWs w = chunk_ws(ws, p.rows, p.n, BF);
   sample_scan_kernel<BF><<<dim3((unsigned)w.chunks, (unsigned)p.rows), kScanThreads, 0, st>>>(p, w);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  sample_draw_kernel<BF><<<dim3((unsigned)p.rows), kThreads, 0, st>>>(p, w, unit);
+  sample_draw_kernel<BF><<<dim3((unsigned)p.rows), kThreads, 0, st>>>(p, w, bits);
   return hipGetLastError();
 }
 

@@ -1,12 +1,16 @@
 """Sampling where rows reach beyond the bins that the kernels count logits in:
-tokens far below the largest logit that are still likely."""
+tokens far below the largest logit that are still likely, prefixes that end among
+very many small weights."""
 
 import math
+from fractions import Fraction
 
+import numpy as np
 import pytest
 import torch
 
 import serving
+from serving import DEV
 from paper_2608_28003_amd import w8a8
 from test_gpu_sample import check, uniform
 
@@ -35,3 +39,39 @@ def test_hot_rows_draw_from_all_their_logits(dt):
     l = (torch.randn((6, 20000), generator=g) * 50.0).to(dt)
     l[:, ::3] = -math.inf
     check(l, uniform(6), t=60.0)
+
+
+@pytest.mark.parametrize("dt,low,t", [(torch.float32, -27.75, 1.0), (torch.bfloat16, -27.75, 1.0),
+                                      (torch.bfloat16, -0.0625, 0.0625 / 27.75), (torch.float32, -0.0625, 0.0625 / 27.75)])
+@pytest.mark.parametrize("n", [1 << 24, 1 << 21])
+def test_nucleus_that_ends_among_millions_of_small_weights(n, dt, low, t):
+    """One likely token at the end, n - 1 equal ones of weight w = 2^-40 before it, and a
+    top_p whose goal lies among them: kept are the largest and the first
+    ceil((top_p Z - 1) / w) of the others, exactly.  Drawn is number floor(u Zk / w).
+
+    u is taken for the middle between two tokens; as binary32 it is within 2^-24 of
+    that, 0.06 tokens at a million of them.  w is within 2^-50 of itself, and sums of
+    n terms within n 2^-53 (2^-29): the tokens' numbers by less than 0.01."""
+    t = float(np.float32(t))
+    w = Fraction(math.exp(low / t))
+    z = 1 + (n - 1) * w
+    p = np.float32(1 - float((n - 1) * w) * 0.6)  # the goal: 40 of 100 small ones
+    kept = math.ceil((Fraction(float(p)) * z - 1) / w)
+    assert 0.1 * n < kept < 0.9 * n
+    zk = 1 + kept * w
+    want = [0, 5, 1000, min(1000000, kept // 2)]
+    u = [float((Fraction(2 * i + 1, 2)) * w / zk) for i in want]
+    # near the border, where a few tokens more or less do not count: kept, and not kept
+    u += [float(kept * Fraction(99, 100) * w / zk), float(kept * Fraction(101, 100) * w / zk), 0.5]
+    l = torch.full((1, n), low, dtype=dt, device=DEV)
+    l[0, n - 1] = 0.0
+    l = l.expand(len(u), n).contiguous()
+    token, prob = w8a8.sample(l, torch.tensor(u, device=DEV), t, 0, float(p))
+    token, prob = token.tolist(), prob.double().tolist()
+    assert token[:4] == want
+    assert abs(token[4] - 0.99 * kept) < 1e-4 * kept and token[5:] == [n - 1, n - 1]
+    # kept is off by n 2^-53 / w tokens at the most, where sums round
+    slack = 2.0 ** -24 + 2.0 ** -40 + n * 2.0 ** -53
+    for i, x in zip(token, prob):
+        exact = float((w if i < n - 1 else 1) / zk)
+        assert abs(x - exact) <= slack * exact
