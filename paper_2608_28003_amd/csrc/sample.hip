@@ -22,8 +22,9 @@
 // The second launch, one workgroup a row, finds the kept prefix and the chunk of
 // the drawn token from counts and sums, and reads that chunk again.  Where the
 // prefix ends inside a bin of several values it sorts that bin's logits.  A row
-// whose prefix ends below the bins, or in one of more than 2048 logits, goes
-// through passes over the row instead.
+// whose prefix ends below the bins among logits that have a weight, or in a bin of
+// several values with more than 2048 logits, goes through passes over the row by that
+// one workgroup instead: 64 rows of 262144 take 1.1 to 1.4 ms then.
 //
 // 64 bf16 rows of 262144: 25 us for the scan, which vector instructions and the atomic
 // additions in LDS bound (33 MB, 1.3 TB/s), 36 for the draw, a chain of steps on one
@@ -838,6 +839,7 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p, C
   uint32_t kept = 0, many = 0;  // many: all logits of the bin
   int listed = -1;        // the bin whose logits are in the list, in order
   bool lost = false;
+  bool all_binned = false;  // known: nothing below the bins has any weight
   // the logits of bin b (m of them) into the list, in order
   auto gather = [&](int b, uint32_t m) {
     if (listed != b) gather_bin<BF>(r, s, count, C, first, b, m);
@@ -875,7 +877,30 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p, C
     take(n_before[0] < k && k <= n_before[0] + n[0], n_before[1] < k && k <= n_before[1] + n[1], k - n_before[0], k - n_before[1]);
     at = s.at;
     value = s.goal;
-    lost = bin == kBins || (!one_value(bin) && kept < many && many > kList);
+    if (bin == kBins) {
+      // Fewer logits than top_k in the bins.  Where all others weigh nothing (a row of which a
+      // grammar allows few tokens, the rest at -inf or at the type's lowest value), what is in the
+      // bins is all that can be drawn, and the row needs no passes: 64 such rows of 262144 took
+      // 1.1 ms with them, and take 0.11 with this look for the largest logit below the bins.
+      const uint32_t edge = first_key(first - (kBins - 2));
+      uint32_t next = 0;
+      for (int64_t i = tid * kVec; i < r.n; i += kBlock) {
+        uint32_t k8[kVec];
+        keys8(r, i, k8);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) next = max(next, k8[e] < edge ? k8[e] : 0u);
+      }
+      next = wave_top(next);
+      __syncthreads();
+      if (lane == 0) s.redu[wave] = next;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) next = max(next, s.redu[i]);
+      lost = weight_call(r, next) > 0.0;
+      all_binned = !lost;
+    } else {
+      lost = !one_value(bin) && kept < many && many > kList;
+    }
   }
   if (a.p_on && !lost) {
     // what the tokens so far weigh
@@ -960,11 +985,12 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(SampleParams p, C
         }
       }
     } else if (bin == kBins) {  // logits below the bins may still be kept
-      lost = weight_call(r, first_key(first - (kBins - 2))) >= a.least;
+      lost = !all_binned && weight_call(r, first_key(first - (kBins - 2))) >= a.least;
       bin = kBins - 1;
       kept = many = 0;
     }
   }
+  if (all_binned && bin == kBins) bin = kBins - 1;
   if (!lost && bin < kBins - 1 && !one_value(bin) && kept > 0 && kept < many) {
     lost = many > kList;
     if (!lost) gather(bin, many);

@@ -75,3 +75,53 @@ def test_nucleus_that_ends_among_millions_of_small_weights(n, dt, low, t):
     for i, x in zip(token, prob):
         exact = float((w if i < n - 1 else 1) / zk)
         assert abs(x - exact) <= slack * exact
+
+
+def masked(rows, n, allowed, dt, seed, low=-math.inf):
+    """Rows of which all but `allowed` logits are `low`."""
+    g = serving.gen(seed)
+    l = torch.full((rows, n), low)
+    for i in range(rows):
+        at = torch.randperm(n, generator=g)[:allowed]
+        l[i, at] = torch.randn(allowed, generator=g) * 3
+    return l.to(dt)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("low", [-math.inf, math.nan, -3e38, -1e4])
+def test_masked_rows(dt, low):
+    """Fewer logits than top_k that can be drawn, with every other filter; and the
+    same with values far below in their place, which count among the top_k."""
+    for n, allowed in ((50, 3), (9000, 20), (40001, 49), (40001, 1)):
+        l, u = masked(6, n, allowed, dt, n, low), uniform(6, n)
+        for a in (dict(k=50), dict(k=50, p=0.9), dict(k=n - 1), dict(k=n - 1, p=0.999999, t=2.0), dict(k=50, m=0.01),
+                  dict(k=50, m=1e-30), dict(k=50, p=0.8, m=0.05), dict(k=50, t=1e4), dict(k=50, t=1e4, m=0.5), dict(k=1)):
+            check(l, u, **a)
+    l[:, ::2] = -math.inf  # far values beside masked ones: kept up to the 50th
+    check(l, uniform(6, 5), k=50, t=1e4)
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("low", [-math.inf, -3e38])
+def test_masked_rows_take_about_as_long_as_others(dt, low):
+    """Both in the same two launches: four times the time leaves room for the look at
+    the rest of the row, passes over the row would take about twenty times."""
+    def ms(l):
+        u = torch.full((l.shape[0],), 0.5, device=DEV)
+        run = lambda: w8a8.sample(l, u, 1.0, 50, 0.9)
+        run()
+        best = math.inf
+        for _ in range(5):
+            e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+            e[0].record()
+            for _ in range(5):
+                run()
+            e[1].record()
+            torch.cuda.synchronize()
+            best = min(best, e[0].elapsed_time(e[1]))
+        return best
+
+    l = torch.randn((64, 262144), generator=serving.gen(1)).to(dt).to(DEV)
+    m = torch.full_like(l, low)
+    m[:, 777:797] = l[:, 777:797]
+    assert ms(m) <= 4 * ms(l)
