@@ -2289,7 +2289,9 @@ w8a8_status w8a8_attn_paged(const void* q, int64_t rows, int64_t ldq, int64_t n_
   p.group = (int)(n_heads / kv->n_kv);
   p.window = (int)std::min<int64_t>(window, 1 << 30);  // no position reaches it
   p.scale_log2 = scale * 1.44269504088896341f;
-  if (std::fabs(p.scale_log2) < FLT_MIN) p.scale_log2 = FLT_MIN;  // 0: as good, and -inf times it is -inf
+  REQUIRE(std::isfinite(p.scale_log2), W8A8_EINVAL, "scale * log2(e) is beyond binary32");
+  // 0: so small that no binary32 score counts, while -inf times it is -inf
+  if (p.scale_log2 == 0.0f) p.scale_log2 = FLT_TRUE_MIN;
   attn_paged_plan(&p, std::min(batch->max_q, rows), batch->max_pages * kv->page);
   if (const size_t need = attn_paged_ws_bytes(p, (int)kv->head_dim)) {
     CHECK_PTR(ws);

@@ -6,6 +6,7 @@ import torch
 import serving
 from serving import DEV
 from paper_2608_28003_amd import w8a8
+from test_gpu_attn_paged import attend
 
 pytestmark = [pytest.mark.gpu,
               pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
@@ -40,3 +41,18 @@ def test_context_beyond_the_largest_table(int8):
     top = 2 * 2.0 ** -8 * max(float(x.abs().max()) for x in kv)
     assert ((out[20:].double() - want.double()).abs() <= 2.0 ** -7 * want.double().abs() + top).all()
     assert (out[20:] != 0).any(-1).all()
+
+
+@pytest.mark.parametrize("int8", [True, False])
+def test_a_scale_of_zero_weighs_all_keys_alike(int8):
+    """... however large the scores are; and one below the normal range as well.
+
+    Queries of 5e35 against rows of 128 values of size 1.5, three of them three times that:
+    products add up to 5e35 * 1.5 * 11 = 1e37, a thirtieth of what binary32 holds.  The sums
+    over INT8 rows are of codes, up to 16 to 20 times their values: a tenth as large there."""
+    large = 5e34 if int8 else 5e35
+    h = serving.Paged([40, 1, 3], [90, 70, 3], 2, 128, 16, int8, seed=9)
+    attend(h, 4, scale=0.0, q_scale=large)
+    attend(h, 4, scale=-0.0, q_scale=large)
+    attend(h, 4, scale=1e-40)
+    attend(h, 4, scale=-1e-40, q_scale=large)

@@ -69,3 +69,12 @@ def test_sample_passes_the_stride_there_is(recorder):
         w8a8.sample(gpu(l), torch.zeros(l.shape[0]))
         a = recorder.calls.pop()
         assert a[1:6] == (l.data_ptr(), w8a8.BF16, *l.shape, ld)
+
+
+def test_attention_refuses_a_scale_that_overflows():
+    """The kernels take scale * log2(e)."""
+    from test_serving_host import FAKE, batch, kv
+
+    for scale in (3e38, -2.4e38):
+        assert w8a8.lib().w8a8_attn_paged(FAKE, 4, 1024, 4, kv(), batch(), 1024, scale, FAKE, 1024, FAKE, 1 << 40,
+                                          None) == w8a8.EINVAL
