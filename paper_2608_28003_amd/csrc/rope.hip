@@ -176,9 +176,9 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p) {
     const int j = h - (key ? p.n_heads : hk);
     const int64_t r = at + ((int64_t)j << p.kv.page_log2);
     if constexpr (I8) {
-      float m = 0.0f;
+      float m = fabsf(x[0]);  // of numbers; NaN where a row has none, so that it stays NaN
 #pragma unroll
-      for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(x[i]));
+      for (int i = 1; i < 16; ++i) m = fmaxf(m, fabsf(x[i]));
       m = fmaxf(m, lane_xor<1>(m));
       m = fmaxf(m, lane_xor<2>(m));
       m = fmaxf(m, lane_xor<4>(m));
