@@ -517,10 +517,25 @@ __global__ __launch_bounds__(kScanThreads, BF ? 4 : 8) void sample_scan_kernel(S
   for (int i = threadIdx.x; i < kBins; i += kScanThreads) hist[i] = 0;
   for (int i = threadIdx.x; i < kFixed; i += kScanThreads) fix[i] = 0;
   float top = NAN;  // of numbers; NaN where there is none
+  bool nan = false;
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) top = fmaxf(top, __uint_as_float(x[v].bits(e)));
+    for (int e = 0; e < kVec; e += 2) {
+      const float f0 = __uint_as_float(x[v].bits(e)), f1 = __uint_as_float(x[v].bits(e + 1));
+      nan |= __builtin_isunordered(f0, f1);
+      top = fmaxf(fmaxf(top, f0), f1);
+    }
+  if (__any(nan)) {  // the maximum of a number and a signalling NaN is NaN: numbers alone
+    top = NAN;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const float f = __uint_as_float(x[v].bits(e));
+        top = f == f ? fmaxf(top, f) : top;
+      }
+  }
   for (int m = 32; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
   if (lane_id() == 0) tops[threadIdx.x >> 6] = top;
   __syncthreads();

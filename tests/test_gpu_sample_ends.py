@@ -125,3 +125,20 @@ def test_masked_rows_take_about_as_long_as_others(dt, low):
     m = torch.full_like(l, low)
     m[:, 777:797] = l[:, 777:797]
     assert ms(m) <= 4 * ms(l)
+
+
+def test_signalling_nan_logits():
+    """NaN of any bits are never drawn and hide no other logit."""
+    g = serving.gen(1)
+    l = torch.randn((4, 9000), generator=g).to(torch.bfloat16)
+    u = uniform(4)
+    bits = l.view(torch.int16)
+    bits[:, ::7], bits[:, 1::7], bits[:, 2::7] = 0x7f81, 0xff81 - 65536, 0x7fc0
+    wide = l.view(torch.int16).int() << 16
+    wide[:, 3::7] = 0x7f800001
+    quiet = lambda x: torch.where(x.isnan(), torch.tensor(math.nan, dtype=x.dtype), x)
+    for x in (l, wide.view(torch.float32)):
+        for a in ({}, dict(t=0.0), dict(k=40), dict(p=0.9), dict(m=0.1), dict(k=8000, p=0.999), dict(t=100.0)):
+            want = check(quiet(x), u, **a)
+            t, k, p, m = (a.get(c, d) for c, d in (("t", 1.0), ("k", 0), ("p", 1.0), ("m", 0.0)))
+            assert torch.equal(w8a8.sample(x.to(DEV), u.to(DEV), t, k, p, m)[0], want), a
