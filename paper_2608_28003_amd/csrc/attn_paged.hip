@@ -821,6 +821,14 @@ __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
         const float4 f = *reinterpret_cast<const float4*>(sc + 32 + 2 * r);
         x[r] *= f.x; x[r + 1] *= f.y; x[r + 2] *= f.z; x[r + 3] *= f.w;
       }
+      if (!whole) {  // a scale that this row does not attend may be NaN
+        const int last = min(pos, hi - 1) - k0 - 4 * g, first = from - k0 - 4 * g;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = 8 * (r >> 2) + (r & 3);
+          x[r] = key >= first && key <= last ? x[r] : 0.0f;
+        }
+      }
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h)

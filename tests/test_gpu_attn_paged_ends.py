@@ -127,3 +127,24 @@ def test_a_prompt_in_chunks_attends_alike(int8):
             bound = 2.0 ** -8 * (a.abs() + b.abs()) * (1 + 2.0 ** -7) + (2 * 2.0 ** -8 + slack) * wide
             assert ((a - b).abs() <= bound).all(), (part, float(((a - b).abs() / bound).max()))
             assert (a != 0).any(-1).all()
+
+
+@pytest.mark.parametrize("d", [128, 256])
+@pytest.mark.parametrize("fresh,heads", [(40, 2), (200, 4), (3, 2)])
+def test_scales_that_are_nan_stay_with_the_tokens_that_attend_them(fresh, heads, d):
+    """INT8: a NaN scale of a key or value reaches the tokens that attend the row, whose
+    results are NaN, and no other: earlier tokens, and later ones behind the window."""
+    h = serving.Paged([fresh, 1], [fresh + 30, 9], 1, d, 16, True, seed=d)
+    q = torch.randn((h.rows, heads, d), generator=serving.gen(2)).to(torch.bfloat16).to(DEV)
+    b, window = h.batch(w8a8), 25
+    good = w8a8.attn_paged(q, h.cache(w8a8), b, window=window)
+    at = fresh + 30 - 1 - fresh // 3  # a position among the new tokens
+    page, slot = int(h.table[0, at // 16]), at % 16
+    pos = torch.arange(30, fresh + 30)
+    sees = (pos >= at) & (pos < at + window)
+    for name in ("sk", "sv"):
+        cache = h.cache(w8a8)
+        getattr(cache, name)[page, 0, slot] = float("nan")
+        out = w8a8.attn_paged(q, cache, b, window=window)
+        assert out[:fresh][sees.to(DEV)].isnan().all()
+        assert torch.equal(out[:fresh][~sees.to(DEV)], good[:fresh][~sees.to(DEV)]) and torch.equal(out[fresh:], good[fresh:])
