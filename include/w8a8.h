@@ -610,12 +610,17 @@ w8a8_status w8a8_kv_read(const w8a8_paged_kv* kv, const w8a8_paged_batch* batch,
    ldq and ldo (multiples of 8).  n_heads: a multiple of n_kv.  window >= 1
    (2^30 and more: none), scale within 2^127 (1 / sqrt(head_dim) as a rule).  Sums
    (of an INT8 cache: of queries times codes, before their scale) and softmax statistics
-   are binary32.  Cached rows past ctx_len, before every new token's window and in pages
-   that are not held are never used.  Of a bf16 cache a non-finite value in a row that one
-   of a sequence's new tokens attends may reach its other new tokens, of an INT8 cache a
-   non-finite scale reaches only those that attend the row.  The same call gives the same
-   bits; how a context is cut into pieces, and so the order of its sums, follows from the
-   lengths of all sequences.
+   are binary32.  The softmax weights are rounded for the product with the values: to 16
+   significant bits (two bf16 values) where a sequence has at most 16 rows, its new tokens
+   times n_heads / n_kv, and to bf16 (by 2^-8 of themselves at most) where it has more, so
+   that a token's result moves by about its own rounding between the two.  Cached rows
+   past ctx_len, before every new token's window and in pages that are not held are never
+   used.  Of a bf16 cache a non-finite value in a row that one of a sequence's new tokens
+   attends may reach its other new tokens, of an INT8 cache a non-finite scale reaches
+   only those that attend the row.  The same call gives the same bits; how a context is cut
+   into pieces, and so the order of its sums, follows from the lengths of all sequences and
+   from the tables' width.  Sequences of more than 16 rows are cut by what the tables can
+   hold: tables no wider than the contexts need are faster.
    ws: w8a8_attn_paged_workspace_bytes(...) bytes of the same sizes, with ctx_max =
    max_pages * page, the positions that the tables can hold (may be NULL when
    that is 0).  Calls that share a workspace must not overlap in time. */

@@ -588,10 +588,15 @@ __device__ __forceinline__ void load_lds16_rows(const char* from, uint32_t off, 
 //
 // 8192 tokens of one prompt, 4 heads of 256, bf16: 160 us, 0.86 PFLOP/s of the pairs
 // that are attended, where a large library product reaches 1.27.  A step of 64 keys takes
-// 7000 cycles of a SIMD: 2 x 1024 of matrix instructions, and between them the reads of
-// LDS, 100 vector instructions and 16 exponentials of 4 cycles and more a wave, and two
-// barriers.  509 tokens over 8192 positions, 16 heads of 128, INT8: 75 us; vector
-// instructions bound it (codes to bf16, two scales, weights).
+// 5100 cycles of a SIMD: 2 x 1024 of matrix instructions (40 %), and between them the reads
+// of LDS, 100 vector instructions and 16 exponentials of 4 cycles and more a wave (all
+// vector instructions: 30 %), and two barriers; the waves wait for those and for loads 27 %
+// of their time, and as long for their turn to issue.  509 tokens over 8192 positions, 16
+// heads of 128, INT8: 73 us, of whose cycles vector instructions (codes to bf16, two scales,
+// weights) take 40 % and matrix instructions 19 %; the waves wait 44 % of their time, and
+// a fifth of LDS' busy cycles are bank conflicts.  INT8 heads of 256 do not fit their
+// registers (19 of 256 spilled, 76 bytes a lane): the prompt of 8192 tokens takes 252 us a
+// call, where bf16 takes 169.
 template <int D, bool I8>
 __global__ __launch_bounds__(512) void attn_tile_kernel(PagedAttnParams p) {
   constexpr int NC = D / 16, NB = D / 32;  // 16-dimension steps of a score, 32-dimension blocks of a result
@@ -1015,6 +1020,12 @@ static constexpr int64_t kRowSlots = 512;
 // few to all (one tile of a piece each: 200 us of the prompt of 8192 tokens instead of
 // 160).  Of 512 keys and more: a piece writes its 128 rows in binary32 and they are read
 // again to be joined.
+//
+// The pieces of tiles follow from what the tables can hold, as the host knows no lengths:
+// the prompt above takes 172 us a call with a table of 8192 positions and 193 with one of
+// 32768 or more, a chunk of 509 tokens over 8192 positions (16 heads on 8 of 128, INT8) 102
+// and 248.  Tiles of few rows cost as much as full ones: 64 sequences of 8 tokens with 4
+// heads of 256 over 2325 to 16384 positions take 255 us, where one token each takes 59.
 static constexpr int kTileSlots = 256, kTilePieceMin = 512;
 
 void attn_paged_plan(PagedAttnParams* p, int64_t max_q, int64_t ctx_max) {
@@ -1022,8 +1033,11 @@ void attn_paged_plan(PagedAttnParams* p, int64_t max_q, int64_t ctx_max) {
   const int64_t span = std::min<int64_t>(std::min<int64_t>(ctx_max, (int64_t)p->window + max_q) + kStep, 1 << 30);
   p->max_q = (int)max_q;
   p->max_rows = (int)std::min<int64_t>(max_q * p->group, kRows);
-  // pieces for each key/value head: the slots, or of more sequences than slots two rounds
-  // of them; more than that fill the CUs whole
+  // Pieces for each key/value head: the slots, or of more sequences than slots two rounds
+  // of them.  More than that are not cut, which serves contexts of like lengths: of 129
+  // sequences of 8 heads, one of 32768 positions among ones of 200 to 500, the long one is one
+  // workgroup a head and takes 422 us.  Nor is it cut where the sequences take all slots
+  // (128 such: 854 us).
   const int64_t rounds = (p->batch.n_seqs * (int64_t)p->kv.n_kv + kRowSlots - 1) / kRowSlots;
   p->row_pieces = p->batch.n_seqs <= kSplitSeqs && rounds <= 2 && span > kPass ? (int)(kRowSlots * rounds / p->kv.n_kv) : 0;
   p->tile_slots = 0;

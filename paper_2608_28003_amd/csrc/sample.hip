@@ -6,9 +6,9 @@
 // and more (the first token always stays).  The token drawn is the first index
 // whose running sum of kept weights exceeds u times their total.
 //
-// The weights and their sums are binary64: a running sum of 262144 binary32
-// weights moves by about 1e-8 with the order of its terms, and as much of the
-// draws would change.
+// The weights are binary64, and their sums binary64 or 64-bit integers of a finer unit
+// than the draws can tell: a running sum of 262144 binary32 weights moves by about 1e-8
+// with the order of its terms, and as much of the draws would change.
 //
 // Two launches.  The first reads every logit once: per chunk of 16384 it counts
 // the logits in 2047 bins from the chunk's largest one down, and adds up weights.
@@ -17,7 +17,8 @@
 // from any usual largest logit over 0 to far below it.  A bf16 bin outside that
 // band is one value, and its weight its count times the value's; the other bins'
 // weights are added as 64-bit integers in units of 2^-48 of the chunk's largest
-// weight, so that no order of the additions matters.
+// weight, and where the row's bins are summed in units of 2^-(62 - log2 n) of the row's
+// (2^-44 of 262144 logits), so that no order of the additions matters.
 //
 // The second launch, one workgroup a row, finds the kept prefix and the chunk of
 // the drawn token from counts and sums, and reads that chunk again.  Where the
@@ -26,11 +27,13 @@
 // several values with more than 2048 logits, goes through passes over the row by that
 // one workgroup instead: 64 rows of 262144 take 1.1 to 1.4 ms then.
 //
-// 64 bf16 rows of 262144: 25 us for the scan, which vector instructions and the atomic
-// additions in LDS bound (33 MB, 1.3 TB/s), 36 for the draw, a chain of steps on one
-// workgroup a row: the row's bins (12 us), the prefix, the chunks' sums (4) and the chunk
-// (4 to 15); 24 more where a prefix ends among the values around 0.  One row: 10 and 20 us.
-// 131 f32 rows of 100003: 28 and 44 us.
+// 64 bf16 rows of 262144: 26 us for the scan (33 MB, 1.3 TB/s), which issues 39 vector and
+// 27 scalar instructions for 64 logits: the vector units are busy half of its cycles, the
+// scalar ones a third, LDS an eighth.  37 for the draw, a chain of steps on one workgroup a
+// row: the row's bins (12 us), the prefix, the chunks' sums (4) and the chunk (4 to 15); 24
+// more where a prefix ends among the values around 0.  One row: 11 and 21 us (with bins from
+// the largest logit to 0 only, 26 for both, but passes over the row where a prefix ends
+// below 0).  131 f32 rows of 100003: 31 and 46 us.
 #include <cmath>
 #include <cstdint>
 
@@ -497,8 +500,8 @@ struct Vec<false> {
   }
 };
 
-// registers: four workgroups a CU for f32 (all of 131 x 100003 logits at once: 28 us); bf16 spills
-// with as few, and 64 x 262144 logits take 28 us instead of 25
+// registers: four workgroups a CU for f32 (all of 131 x 100003 logits at once); bf16 spills with
+// as few, and 64 x 262144 logits took 28 us where they took 25 with more
 template <bool BF>
 __global__ __launch_bounds__(kScanThreads, BF ? 4 : 8) void sample_scan_kernel(SampleParams p, ChunkWs ws) {
   constexpr int V = kChunk / kScanThreads / kVec, kFixed = BF ? 2 * kBand : kBins;
