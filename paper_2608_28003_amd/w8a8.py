@@ -1041,8 +1041,8 @@ def attn_paged(q, cache: PagedKV, batch: PagedBatch, window=None, scale=None, ou
         if ws is None:
             ws = _empty(attn_paged_workspace_bytes(rows, heads, kv.n_kv, d, b.n_seqs, b.max_q,
                                                    b.max_pages * kv.page, window), q.device)
-        elif ws.device != q.device:
-            raise ValueError("ws must be on q's device")
+        elif ws.device != q.device or not ws.is_contiguous():
+            raise ValueError("ws must be contiguous and on q's device")
         _check(lib().w8a8_attn_paged(q.data_ptr(), rows, ldq, heads, ctypes.byref(kv), ctypes.byref(b),
                                      1 << 30 if window is None else window,
                                      d ** -0.5 if scale is None else scale, out.data_ptr(), ldo,
@@ -1083,8 +1083,8 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None, 
             else _need(prob, "prob", torch.float32, device, (rows,))
         if ws is None:
             ws = _empty(lib().w8a8_sample_workspace_bytes(rows, n, dt), device)
-        elif ws.device != device:
-            raise ValueError("ws must be on the logits' device")
+        elif ws.device != device or not ws.is_contiguous():
+            raise ValueError("ws must be contiguous and on the logits' device")
         _check(lib().w8a8_sample(ctypes.byref(d), logits.data_ptr(), dt, rows, n, ld, u.data_ptr(),
                                  out.data_ptr(), prob.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), st))
     return out, prob

@@ -26,6 +26,9 @@ class Recorder:
         self.calls.append(a)
         return 0
 
+    w8a8_attn_paged_workspace_bytes = w8a8_sample_workspace_bytes
+    w8a8_attn_paged = w8a8_sample
+
 
 class Stream:
     def __init__(self, *a):
@@ -78,3 +81,24 @@ def test_attention_refuses_a_scale_that_overflows():
     for scale in (3e38, -2.4e38):
         assert w8a8.lib().w8a8_attn_paged(FAKE, 4, 1024, 4, kv(), batch(), 1024, scale, FAKE, 1024, FAKE, 1 << 40,
                                           None) == w8a8.EINVAL
+
+
+def test_workspaces_are_memory_of_their_size(recorder):
+    """One byte expanded, or every second byte, has as many elements as a workspace of
+    that size, but not its memory."""
+    logits, u = gpu(torch.zeros(2, 100, dtype=torch.bfloat16)), torch.zeros(2)
+    q = gpu(torch.zeros(2, 4, 256, dtype=torch.bfloat16))
+    cache = w8a8.PagedKV.empty(2, 16, device="cpu")
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32)
+    batch = w8a8.PagedBatch(ints([0, 1]), ints(0, 2), ints(20), 2)
+    one = torch.zeros(1, dtype=torch.uint8)
+    for ws in (one.expand(1 << 20), torch.zeros(1 << 10, dtype=torch.uint8)[::2], torch.zeros(64, 64).t()[1:]):
+        with pytest.raises(ValueError):
+            w8a8.sample(logits, u, ws=ws)
+        with pytest.raises(ValueError):
+            w8a8.attn_paged(q, cache, batch, ws=ws)
+    assert recorder.calls == []
+    ws = torch.zeros(1 << 10, dtype=torch.int32)
+    w8a8.sample(logits, u, ws=ws)
+    w8a8.attn_paged(q, cache, batch, ws=ws)
+    assert [a[-3:-1] for a in recorder.calls] == [(ws.data_ptr(), 4 << 10)] * 2
