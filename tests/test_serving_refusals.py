@@ -96,9 +96,9 @@ def test_workspaces_are_memory_of_their_size(recorder):
         with pytest.raises(ValueError):
             w8a8.sample(logits, u, ws=ws)
         with pytest.raises(ValueError):
-            w8a8.attn_paged(q, cache, batch, ws=ws)
+            w8a8.attn_paged(q, cache, batch, out=q, ws=ws)
     assert recorder.calls == []
     ws = torch.zeros(1 << 10, dtype=torch.int32)
     w8a8.sample(logits, u, ws=ws)
-    w8a8.attn_paged(q, cache, batch, ws=ws)
+    w8a8.attn_paged(q, cache, batch, out=q, ws=ws)
     assert [a[-3:-1] for a in recorder.calls] == [(ws.data_ptr(), 4 << 10)] * 2
